@@ -274,6 +274,105 @@ int nsml_decompress_accumulate(nsml_ctx *ctx, const uint32_t *idx, const void *v
  * scheduling.  Synchronises the device.  NSML_EINVAL before the first compress. */
 int nsml_last_l2norm(nsml_ctx *ctx, double *total, double *per_bucket);
 
+/* ------------------------------------------------------------------ the 8-bit layer
+ *
+ * What a worker runs before it has a gradient to reduce: the layers whose weight gradients
+ * nsml_compress sends, with activations in 8 bits.  No context: every function enqueues on `stream`
+ * of the current device, allocates nothing, keeps nothing, and may run beside any other call.
+ *
+ *   types     NSML_F32, NSML_BF16, NSML_F16: all matrices marked "type" of one call have the same;
+ *             arithmetic is in binary32, rounded once when a result of 16 bits is stored
+ *   matrices  rows x cols, neighbours of a row side by side, `ld` elements from row to row
+ *             (ld >= cols); any alignment of the type; rows == 0 is allowed (what has so many rows may be NULL then)
+ *   rows in 8 bits (q, scale)     the operands of products.  value = q * scale[row], q in [-127, 127].
+ *             Coding takes scale = absmax / 127 of the row and q = rint(t * (127 / absmax)).  A row whose
+ *             absmax is below 2^-112 has scale 0 and codes 0; a row that holds an infinity or NaN has scale
+ *             NaN and codes 0, so that what is made from it is NaN and no other row is touched.
+ *   checkpoints (nsml_ckpt8)      what the backward pass keeps: every 32 neighbours of a row share a power of
+ *             two.  value = q * 2^(e - 127), e = floor(log2 absmax) - 6 + 127 (at least 1), q = rint(x / 2^(e - 127))
+ *             held to [-127, 127].  A block with an infinity or NaN has e = 255 and codes 0 and reads as NaN.
+ *             Values are exact in bfloat16, so a weight gradient takes them without another rounding.
+ *   code matrices   16-byte aligned, ld a multiple of 16; the bytes of a row up to the next multiple of 16
+ *             belong to it (their contents are never used as values, and may be overwritten)
+ * NSML_EINVAL: a null pointer, an unknown type, cols == 0, ld < cols, a code matrix or pointer that is not aligned
+ * as above; NSML_ECAP: cols beyond the limit named; NSML_EHIP: the launch failed.  Buffers of one call
+ * must not overlap where one of them is written, unless said otherwise. */
+
+#define NSML_F32  0
+#define NSML_BF16 1
+#define NSML_F16  2
+#define NSML_Q8_MAX_COLS   131072u   /* longest row in 8 bits: sums of 127 * 127 fit 32 bits */
+#define NSML_NORM_MAX_COLS  32768u   /* widest row of a norm */
+
+typedef struct nsml_ckpt8 {
+    int8_t *q;           /* rows x cols codes, ldq bytes from row to row */
+    uint8_t *e;          /* rows x ceil(cols / 32) exponents, lde bytes from row to row */
+    uint64_t ldq, lde;
+} nsml_ckpt8;
+
+/* Rows of x (type), each column times col_scale (dev, float[cols], or NULL), in 8 bits: weights by output
+ * channel, activations and gradients by token.  scale: dev, out, float[rows].  cols <= NSML_Q8_MAX_COLS. */
+int nsml_q8_rows(const void *x, int type, uint64_t ldx, uint64_t rows, uint32_t cols, const float *col_scale,
+                 int8_t *q, uint64_t ldq, float *scale, void *stream);
+/* Back: out (type) = q * scale[row]; scale NULL: 1. */
+int nsml_q8_values(const int8_t *q, uint64_t ldq, const float *scale, uint64_t rows, uint32_t cols,
+                   void *out, int type, uint64_t ldo, void *stream);
+
+/* c[i, j] (type, m x n) = a_scale[i] * b_scale[j] * sum_k a[i, k] * b[j, k] + bias[j]: a product with weights held by
+ * output channel (n x k).  The sum is exact.  b_scale, bias (dev, float[n]) may be NULL (1 and 0); k <=
+ * NSML_Q8_MAX_COLS.  The gradient of the data is the same product: rows of (dc times b_scale by columns) with the
+ * codes of b the other way round (k x n) and b_scale NULL. */
+int nsml_q8_matmul(const int8_t *a, uint64_t lda, const float *a_scale, const int8_t *b, uint64_t ldb,
+                   const float *b_scale, const float *bias, uint64_t m, uint32_t n, uint32_t k,
+                   void *c, int type, uint64_t ldc, void *stream);
+
+/* x (type) as a checkpoint, and back.  A value that the type cannot hold is rounded as any other. */
+int nsml_ckpt8_pack(const void *x, int type, uint64_t ldx, uint64_t rows, uint32_t cols, const nsml_ckpt8 *out,
+                    void *stream);
+int nsml_ckpt8_unpack(const nsml_ckpt8 *x, uint64_t rows, uint32_t cols, void *out, int type, uint64_t ldo,
+                      void *stream);
+
+/* Weight gradient of a layer whose input is held as a checkpoint:
+ * dw[j, i] (float, n x k) = add[j, i] + col_scale[i] * sum over rows t of dy[t, j] * x[t, i].
+ *   dy         dev, type, rows x n     x  checkpoint, rows x k
+ *   col_scale  dev, float[k], or NULL  (a norm's gamma, where x is the normalized value)
+ *   add        dev, float, n x k with dw's ld, or NULL; may be dw itself (a sum over micro-batches)
+ *   work       dev, 16-byte aligned, nsml_ckpt8_wgrad_work(rows, n, k) bytes (may be 0), not kept
+ * Products are exact, sums are in binary32 in an order that sizes alone decide.  rows == 0 gives add, or zeros.
+ * dw may be a part of the flat gradient that nsml_compress takes. */
+uint64_t nsml_ckpt8_wgrad_work(uint64_t rows, uint32_t n, uint32_t k);
+int nsml_ckpt8_wgrad(const void *dy, int type, uint64_t lddy, const nsml_ckpt8 *x, const float *col_scale,
+                     uint64_t rows, uint32_t n, uint32_t k, const float *add, float *dw, uint64_t lddw,
+                     void *work, uint64_t work_bytes, void *stream);
+
+/* Root-mean-square norm with the residual's addition, in 8 bits:
+ *   h = x + residual (type, rounded; both NULL: h is x)       rstd = 1 / sqrt(mean of h^2 over the row + eps)
+ *   (q, scale) = rows of gamma * h * rstd                     xhat = checkpoint of h * rstd (or NULL)
+ * gamma: dev, float[cols], or NULL for 1.  rstd: dev, out, float[rows].  Codes do not depend on how the mean was rounded:
+ * they are those of gamma * h, and rstd goes into the scale.  cols <= NSML_NORM_MAX_COLS. */
+int nsml_rmsnorm_q8(const void *x, uint64_t ldx, const void *residual, uint64_t ldr, const float *gamma, float eps,
+                    int type, uint64_t rows, uint32_t cols, void *h, uint64_t ldh, int8_t *q, uint64_t ldq,
+                    float *scale, float *rstd, const nsml_ckpt8 *xhat, void *stream);
+/* Its gradient: with g = dy * gamma (dy: gradient of gamma * h * rstd),
+ *   dx = rstd * (g - xhat * mean(g * xhat)) + dres            gradient of x and of residual; dres (type) or NULL:
+ *                                                             what reaches h by the residual stream
+ *   dgamma[i] = sum over rows of dy * xhat                    dev, out, float[cols], or NULL
+ * work: dev, 16-byte aligned, nsml_rmsnorm_backward_work(rows, cols) bytes, needed for dgamma.  rows == 0: dgamma = 0. */
+uint64_t nsml_rmsnorm_backward_work(uint64_t rows, uint32_t cols);
+int nsml_rmsnorm_backward(const void *dy, uint64_t lddy, const nsml_ckpt8 *xhat, const float *rstd, const float *gamma,
+                          const void *dres, uint64_t lddres, int type, uint64_t rows, uint32_t cols,
+                          void *dx, uint64_t lddx, float *dgamma, void *work, uint64_t work_bytes, void *stream);
+
+/* Gated activation a = gate / (1 + exp(-gate)) * up: (q, scale) = rows of a; gate_ckpt, up_ckpt, act_ckpt: checkpoints of
+ * gate, up and a, each may be NULL.  cols <= NSML_Q8_MAX_COLS. */
+int nsml_swiglu_q8(const void *gate, uint64_t ldg, const void *up, uint64_t ldu, int type, uint64_t rows, uint32_t cols,
+                   int8_t *q, uint64_t ldq, float *scale, const nsml_ckpt8 *gate_ckpt, const nsml_ckpt8 *up_ckpt,
+                   const nsml_ckpt8 *act_ckpt, void *stream);
+/* Its gradient from the checkpoints: s = 1 / (1 + exp(-gate)), dup = da * gate * s,
+ * dgate = da * up * s * (1 + gate * (1 - s)).  dgate and dup may be parts of one matrix. */
+int nsml_swiglu_backward(const void *da, uint64_t ldda, const nsml_ckpt8 *gate, const nsml_ckpt8 *up, int type,
+                         uint64_t rows, uint32_t cols, void *dgate, uint64_t lddg, void *dup, uint64_t lddu, void *stream);
+
 /* ------------------------------------------------------------------ measurement */
 
 #define NSML_MAX_KERNELS 32

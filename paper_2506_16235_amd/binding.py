@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional, Sequence, Tuple
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
@@ -441,3 +441,314 @@ def compress_pruned(ctx: Context, grad, residual, weights, bucket_off, ratio, bi
 
 def decompress(ctx: Context, idx, val, scales, n, bucket_off, ratio, bits, out=None):
     return ctx.decompress(idx, val, scales, n, bucket_off, ratio, bits, out)
+
+
+# ----------------------------------------------------------------------- the 8-bit layer
+
+Q8_MAX_COLS, NORM_MAX_COLS = 131072, 32768
+
+
+class _CkptArg(C.Structure):
+    _fields_ = [("q", _vp), ("e", _vp), ("ldq", _u64), ("lde", _u64)]
+
+
+_f32c, _ck = C.c_float, C.POINTER(_CkptArg)
+for _name, _args in {
+    "nsml_q8_rows": [_vp, _i32, _u64, _u64, _u32, _vp, _vp, _u64, _vp, _vp],
+    "nsml_q8_values": [_vp, _u64, _vp, _u64, _u32, _vp, _i32, _u64, _vp],
+    "nsml_q8_matmul": [_vp, _u64, _vp, _vp, _u64, _vp, _vp, _u64, _u32, _u32, _vp, _i32, _u64, _vp],
+    "nsml_ckpt8_pack": [_vp, _i32, _u64, _u64, _u32, _ck, _vp],
+    "nsml_ckpt8_unpack": [_ck, _u64, _u32, _vp, _i32, _u64, _vp],
+    "nsml_ckpt8_wgrad_work": [_u64, _u32, _u32],
+    "nsml_ckpt8_wgrad": [_vp, _i32, _u64, _ck, _vp, _u64, _u32, _u32, _vp, _vp, _u64, _vp, _u64, _vp],
+    "nsml_rmsnorm_q8": [_vp, _u64, _vp, _u64, _vp, _f32c, _i32, _u64, _u32, _vp, _u64, _vp, _u64, _vp, _vp, _ck, _vp],
+    "nsml_rmsnorm_backward_work": [_u64, _u32],
+    "nsml_rmsnorm_backward": [_vp, _u64, _ck, _vp, _vp, _vp, _u64, _i32, _u64, _u32, _vp, _u64, _vp, _vp, _u64, _vp],
+    "nsml_swiglu_q8": [_vp, _u64, _vp, _u64, _i32, _u64, _u32, _vp, _u64, _vp, _ck, _ck, _ck, _vp],
+    "nsml_swiglu_backward": [_vp, _u64, _ck, _ck, _i32, _u64, _u32, _vp, _u64, _vp, _u64, _vp],
+}.items():
+    getattr(_lib, _name).argtypes = _args
+    getattr(_lib, _name).restype = _u64 if _name.endswith("_work") else _i32
+
+
+class Q8(NamedTuple):
+    """A matrix in 8 bits by rows: value = q * scale[row].  q: int8 [rows, cols], its row stride a multiple of 16;
+    scale: float32 [rows], or None for 1 (the second operand of q8_matmul only)."""
+    q: torch.Tensor
+    scale: Optional[torch.Tensor]
+
+
+class Ckpt8(NamedTuple):
+    """A matrix as a checkpoint: value = q * 2 ** (e - 127), one e (uint8 [rows, ceil(cols / 32)]) for 32 neighbours
+    of a row.  q as in Q8."""
+    q: torch.Tensor
+    e: torch.Tensor
+
+
+class NormQ8(NamedTuple):
+    h: torch.Tensor             # x + residual (x itself without a residual)
+    y: Q8                       # gamma * h * rstd
+    rstd: torch.Tensor          # float32 [rows]
+    xhat: Optional[Ckpt8]       # h * rstd
+
+
+class GluQ8(NamedTuple):
+    a: Q8                       # the activation
+    gate: Optional[Ckpt8]
+    up: Optional[Ckpt8]
+    held: Optional[Ckpt8]       # the activation again, for the weight gradient of the product that takes it
+
+
+_TYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_F32_ONLY, _I8_ONLY, _U8_ONLY = torch.float32, torch.int8, torch.uint8
+
+
+def _matrix(name, t, dev, dtype=None, rows=None, cols=None):
+    """-> (address, elements from row to row, rows, cols) of a matrix whose rows are contiguous."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a torch tensor")
+    if t.dim() != 2:
+        raise ValueError(f"{name} has {t.dim()} dimensions, needs 2")
+    if t.device != dev:
+        raise ValueError(f"{name} is on {t.device}, not on {dev}")
+    if (t.dtype not in _TYPE) if dtype is None else (t.dtype != dtype):
+        raise ValueError(f"{name} has dtype {t.dtype}")
+    r, c = t.shape
+    if (rows is not None and r != rows) or (cols is not None and c != cols):
+        raise ValueError(f"{name} is {r} x {c}, needs {r if rows is None else rows} x {c if cols is None else cols}")
+    if c == 0:
+        raise ValueError(f"{name} has no columns")
+    ld, side = t.stride()
+    if (side != 1 and c > 1 and r) or (ld < c and r > 1):
+        raise ValueError(f"{name} has strides {t.stride()}: rows must be contiguous and must not overlap")
+    return t.data_ptr(), max(ld, c), r, c
+
+
+def _vector(name, t, dev, n):
+    """-> address of a float32 vector, or None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.device != dev or t.dtype != _F32_ONLY or t.dim() != 1 or t.shape[0] != n \
+            or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous float32 vector of {n} elements on {dev}")
+    return t.data_ptr()
+
+
+def _codes(name, t, dev, rows=None, cols=None):
+    """_matrix of int8 codes: 16-byte aligned rows that own their bytes up to the next multiple of 16."""
+    at, ld, r, c = _matrix(name, t, dev, _I8_ONLY, rows, cols)
+    room = (c + 15) // 16 * 16
+    if r <= 1:
+        ld = room
+    if ld % 16 or at % 16:
+        raise ValueError(f"{name}: rows of codes must start at multiples of 16 bytes (strides {t.stride()})")
+    if room != c and r and t.storage_offset() + (r - 1) * ld + room > t.untyped_storage().nbytes():
+        raise ValueError(f"{name}: the last row of codes must own its bytes up to the next multiple of 16")
+    return at, ld, r, c
+
+
+def _rows_of(name, x, dev, rows=None, cols=None):
+    """-> (address of the codes, ld, rows, cols, address of the scales)."""
+    if not isinstance(x, Q8):
+        raise ValueError(f"{name} must be a Q8")
+    at, ld, r, c = _codes(name + ".q", x.q, dev, rows, cols)
+    return at, ld, r, c, _vector(name + ".scale", x.scale, dev, r)
+
+
+def _ckpt(name, x, dev, rows=None, cols=None):
+    """-> (argument, rows, cols) of a checkpoint."""
+    if not isinstance(x, Ckpt8):
+        raise ValueError(f"{name} must be a Ckpt8")
+    at, ld, r, c = _codes(name + ".q", x.q, dev, rows, cols)
+    e, lde, _, _ = _matrix(name + ".e", x.e, dev, _U8_ONLY, r, (c + 31) // 32)
+    return _CkptArg(at, e, ld, lde), r, c
+
+
+def _new_codes(rows: int, cols: int, dev) -> torch.Tensor:
+    ld = (cols + 15) // 16 * 16
+    q = torch.empty((rows, ld), dtype=torch.int8, device=dev)
+    return q if ld == cols else q[:, :cols]
+
+
+def _new_q8(rows, cols, dev) -> Q8:
+    return Q8(_new_codes(rows, cols, dev), torch.empty(rows, dtype=torch.float32, device=dev))
+
+
+def _new_ckpt(rows, cols, dev) -> Ckpt8:
+    return Ckpt8(_new_codes(rows, cols, dev), torch.empty((rows, (cols + 31) // 32), dtype=torch.uint8, device=dev))
+
+
+def _device_of(name, t) -> torch.device:
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise ValueError(f"{name} must be a tensor on a GPU")
+    return t.device
+
+
+def _enqueue(dev, name, *args):
+    """One call of the library on torch's current stream of the device."""
+    fn = getattr(_lib, name)
+    if torch._C._cuda_getDevice() == dev.index:
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
+    if rc != OK:
+        _check(rc, name)
+
+
+def q8_rows(x: torch.Tensor, col_scale: Optional[torch.Tensor] = None, out: Optional[Q8] = None) -> Q8:
+    """The rows of x (times col_scale by columns) in 8 bits: weights by output channel, tokens."""
+    dev = _device_of("x", x)
+    at, ld, m, k = _matrix("x", x, dev)
+    col = _vector("col_scale", col_scale, dev, k)
+    if out is None:
+        out = _new_q8(m, k, dev)
+    q, ldq, _, _, s = _rows_of("out", out, dev, m, k)
+    _enqueue(dev, "nsml_q8_rows", at, _TYPE[x.dtype], ld, m, k, col, q, ldq, s)
+    return out
+
+
+def q8_values(x: Q8, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values that 8-bit rows stand for."""
+    dev = _device_of("x.q", x.q)
+    q, ldq, m, k, s = _rows_of("x", x, dev)
+    if out is None:
+        out = torch.empty((m, k), dtype=dtype, device=dev)
+    at, ld, _, _ = _matrix("out", out, dev, None, m, k)
+    _enqueue(dev, "nsml_q8_values", q, ldq, s, m, k, at, _TYPE[out.dtype], ld)
+    return out
+
+
+def q8_matmul(a: Q8, b: Q8, dtype: torch.dtype = torch.bfloat16, bias: Optional[torch.Tensor] = None,
+              out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """a (m x k) times b (n x k, weights by output channel) transposed, plus bias (float32 [n]); the sum is exact."""
+    dev = _device_of("a.q", a.q)
+    qa, lda, m, k, sa = _rows_of("a", a, dev)
+    qb, ldb, n, _, sb = _rows_of("b", b, dev, None, k)
+    if sa is None:
+        raise ValueError("a.scale is required")
+    v = _vector("bias", bias, dev, n)
+    if out is None:
+        out = torch.empty((m, n), dtype=dtype, device=dev)
+    at, ld, _, _ = _matrix("out", out, dev, None, m, n)
+    _enqueue(dev, "nsml_q8_matmul", qa, lda, sa, qb, ldb, sb, v, m, n, k, at, _TYPE[out.dtype], ld)
+    return out
+
+
+def ckpt8_pack(x: torch.Tensor, out: Optional[Ckpt8] = None) -> Ckpt8:
+    """x as a checkpoint in 8 bits."""
+    dev = _device_of("x", x)
+    at, ld, m, k = _matrix("x", x, dev)
+    if out is None:
+        out = _new_ckpt(m, k, dev)
+    _enqueue(dev, "nsml_ckpt8_pack", at, _TYPE[x.dtype], ld, m, k, _ckpt("out", out, dev, m, k)[0])
+    return out
+
+
+def ckpt8_unpack(x: Ckpt8, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values that a checkpoint stands for."""
+    dev = _device_of("x.q", x.q)
+    arg, m, k = _ckpt("x", x, dev)
+    if out is None:
+        out = torch.empty((m, k), dtype=dtype, device=dev)
+    at, ld, _, _ = _matrix("out", out, dev, None, m, k)
+    _enqueue(dev, "nsml_ckpt8_unpack", arg, m, k, at, _TYPE[out.dtype], ld)
+    return out
+
+
+def ckpt8_wgrad(dy: torch.Tensor, x: Ckpt8, col_scale: Optional[torch.Tensor] = None,
+                add: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """float32 [n, k]: add + col_scale * (dy transposed times x).  out may be a view of the flat gradient that compress
+    takes, and may be add (a sum over micro-batches)."""
+    dev = _device_of("dy", dy)
+    at, ld, m, n = _matrix("dy", dy, dev)
+    arg, _, k = _ckpt("x", x, dev, m)
+    col = _vector("col_scale", col_scale, dev, k)
+    if out is None:
+        out = torch.empty((n, k), dtype=torch.float32, device=dev)
+    w, ldw, _, _ = _matrix("out", out, dev, _F32_ONLY, n, k)
+    base = None
+    if add is not None:
+        base, lda, _, _ = _matrix("add", add, dev, _F32_ONLY, n, k)
+        if n == 1:
+            lda = ldw
+        if lda != ldw:
+            raise ValueError("add and out must have the same row stride")
+    need = _lib.nsml_ckpt8_wgrad_work(m, n, k)
+    work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    _enqueue(dev, "nsml_ckpt8_wgrad", at, _TYPE[dy.dtype], ld, arg, col, m, n, k, base, w, ldw,
+             None if work is None else work.data_ptr(), need)
+    return out
+
+
+def rmsnorm_q8(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, eps: float = 1e-5,
+               residual: Optional[torch.Tensor] = None, checkpoint: bool = False) -> NormQ8:
+    """RMS norm of x (+ residual) with its output in 8 bits; checkpoint: the normalized values for the backward pass."""
+    dev = _device_of("x", x)
+    at, ld, m, k = _matrix("x", x, dev)
+    h, r, ldr, ha, ldh = x, None, 0, None, 0
+    if residual is not None:
+        r, ldr, _, _ = _matrix("residual", residual, dev, x.dtype, m, k)
+        h = torch.empty((m, k), dtype=x.dtype, device=dev)
+        ha, ldh = h.data_ptr(), k
+    g = _vector("gamma", gamma, dev, k)
+    y = _new_q8(m, k, dev)
+    rstd = torch.empty(m, dtype=torch.float32, device=dev)
+    xhat = _new_ckpt(m, k, dev) if checkpoint else None
+    _enqueue(dev, "nsml_rmsnorm_q8", at, ld, r, ldr, g, eps, _TYPE[x.dtype], m, k, ha, ldh, y.q.data_ptr(),
+             (k + 15) // 16 * 16, y.scale.data_ptr(), rstd.data_ptr(), None if xhat is None else _ckpt("xhat", xhat, dev)[0])
+    return NormQ8(h, y, rstd, xhat)
+
+
+def rmsnorm_backward(dy: torch.Tensor, xhat: Ckpt8, rstd: torch.Tensor, gamma: Optional[torch.Tensor] = None,
+                     dres: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                     dgamma: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """-> (gradient of x and of the residual, gradient of gamma).  dres: what reaches the sum by the residual stream."""
+    dev = _device_of("dy", dy)
+    at, ld, m, k = _matrix("dy", dy, dev)
+    arg, _, _ = _ckpt("xhat", xhat, dev, m, k)
+    rs, g = _vector("rstd", rstd, dev, m), _vector("gamma", gamma, dev, k)
+    if rs is None:
+        raise ValueError("rstd is required")
+    d, ldd = None, 0
+    if dres is not None:
+        d, ldd, _, _ = _matrix("dres", dres, dev, dy.dtype, m, k)
+    if out is None:
+        out = torch.empty((m, k), dtype=dy.dtype, device=dev)
+    o, ldo, _, _ = _matrix("out", out, dev, dy.dtype, m, k)
+    if dgamma is None:
+        dgamma = torch.empty(k, dtype=torch.float32, device=dev)
+    need = _lib.nsml_rmsnorm_backward_work(m, k)
+    work = torch.empty(need, dtype=torch.uint8, device=dev)
+    _enqueue(dev, "nsml_rmsnorm_backward", at, ld, arg, rs, g, d, ldd, _TYPE[dy.dtype], m, k, o, ldo,
+             _vector("dgamma", dgamma, dev, k), work.data_ptr(), need)
+    return out, dgamma
+
+
+def swiglu_q8(gate: torch.Tensor, up: torch.Tensor, checkpoint: bool = False) -> GluQ8:
+    """gate / (1 + exp(-gate)) * up in 8 bits by rows; checkpoint: gate, up and the result for the backward pass."""
+    dev = _device_of("gate", gate)
+    g, ldg, m, k = _matrix("gate", gate, dev)
+    u, ldu, _, _ = _matrix("up", up, dev, gate.dtype, m, k)
+    a = _new_q8(m, k, dev)
+    held = [_new_ckpt(m, k, dev) for _ in range(3)] if checkpoint else [None] * 3
+    args = [None if c is None else _ckpt("checkpoint", c, dev)[0] for c in held]
+    _enqueue(dev, "nsml_swiglu_q8", g, ldg, u, ldu, _TYPE[gate.dtype], m, k, a.q.data_ptr(), (k + 15) // 16 * 16,
+             a.scale.data_ptr(), *args)
+    return GluQ8(a, *held)
+
+
+def swiglu_backward(da: torch.Tensor, gate: Ckpt8, up: Ckpt8, dgate: Optional[torch.Tensor] = None,
+                    dup: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """-> gradients of gate and up.  dgate and dup may be halves of one matrix."""
+    dev = _device_of("da", da)
+    at, ld, m, k = _matrix("da", da, dev)
+    kg, ku = _ckpt("gate", gate, dev, m, k)[0], _ckpt("up", up, dev, m, k)[0]
+    if dgate is None:
+        dgate = torch.empty((m, k), dtype=da.dtype, device=dev)
+    if dup is None:
+        dup = torch.empty((m, k), dtype=da.dtype, device=dev)
+    g, ldg, _, _ = _matrix("dgate", dgate, dev, da.dtype, m, k)
+    u, ldu, _, _ = _matrix("dup", dup, dev, da.dtype, m, k)
+    _enqueue(dev, "nsml_swiglu_backward", at, ld, kg, ku, _TYPE[da.dtype], m, k, g, ldg, u, ldu)
+    return dgate, dup

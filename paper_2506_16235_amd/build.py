@@ -15,6 +15,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
+LAYER8 = os.path.join(CSRC, "layer8")           # the 8-bit layer, a translation unit per kind of kernel
+LAYER8_UNITS = ("rows", "products", "wgrad")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libnsml.so")
 
@@ -35,15 +37,24 @@ def build(verbose: bool = True) -> str:
     """Compile every source, always (callers decide when a rebuild is needed)."""
     obj_ctl = os.path.join(CSRC, "nsml_ctl.o")
     obj_hip = os.path.join(CSRC, "nsml_kernels.o")
-    cmds = [
+    units = [(os.path.join(LAYER8, u + ".hip"), os.path.join(LAYER8, u + ".o")) for u in LAYER8_UNITS]
+    compiles = [
         ["gcc", *C_FLAGS, "-I", INCLUDE, "-c", os.path.join(CSRC, "nsml_ctl.c"), "-o", obj_ctl],
         [HIPCC, *HIP_FLAGS, "-I", INCLUDE, "-c", os.path.join(CSRC, "nsml_kernels.hip"), "-o", obj_hip],
-        [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", obj_ctl, obj_hip, "-o", LIB + ".tmp", "-lm"],
+        *[[HIPCC, *HIP_FLAGS, "-I", INCLUDE, "-c", src, "-o", obj] for src, obj in units],
     ]
-    for cmd in cmds:
+    running = []
+    for cmd in compiles:
         if verbose:
             print(" ".join(cmd), flush=True)
-        subprocess.check_call(cmd)
+        running.append(subprocess.Popen(cmd))
+    failed = [cmd for cmd, p in zip(compiles, running) if p.wait()]
+    if failed:
+        raise subprocess.CalledProcessError(1, failed[0])
+    link = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", obj_ctl, obj_hip, *[obj for _, obj in units], "-o", LIB + ".tmp", "-lm"]
+    if verbose:
+        print(" ".join(link), flush=True)
+    subprocess.check_call(link)
     os.replace(LIB + ".tmp", LIB)
     return LIB
 

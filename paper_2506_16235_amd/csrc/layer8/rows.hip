@@ -1,0 +1,569 @@
+/*
+ * The 8-bit layer's passes over rows: coding by rows, the norm and its gradient, the gated activation and its
+ * gradient, checkpoints written and read.
+ *
+ * All of them are bound by memory (1 to 6 operations per byte): every element is read once, what a row's absmax,
+ * sum or mean is needed for waits in registers, and what is written goes out in the same kernel.
+ */
+#include "layer8.hpp"
+
+namespace {
+
+/* ---------------------------------------------------------------- reductions */
+
+template <int CTRL> __device__ __forceinline__ uint32_t dpp(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xF, 0xF, true);
+}
+/* Over the 64 lanes, in one order: neighbours, pairs, halves and mirror images of 16, then the four sixteens. */
+template <typename F> __device__ __forceinline__ uint32_t wave_all(uint32_t v, F f)
+{
+    v = f(v, dpp<0xB1>(v));
+    v = f(v, dpp<0x4E>(v));
+    v = f(v, dpp<0x141>(v));
+    v = f(v, dpp<0x140>(v));
+    const uint32_t a = __builtin_amdgcn_readlane(v, 0), b = __builtin_amdgcn_readlane(v, 16);
+    const uint32_t c = __builtin_amdgcn_readlane(v, 32), d = __builtin_amdgcn_readlane(v, 48);
+    return f(f(a, b), f(c, d));
+}
+__device__ __forceinline__ uint32_t max_of(uint32_t a, uint32_t b) { return max(a, b); }
+__device__ __forceinline__ uint32_t sum_of(uint32_t a, uint32_t b) { return to_bits(from_bits(a) + from_bits(b)); }
+
+/* ---------------------------------------------------------------- rows that are coded as a whole */
+
+/* T threads hold a row, V times eight neighbours each; V == 0: rows wider than registers hold are read twice.
+ * OP: load() gives the values to code and adds to the row's sum, done() gets the sum and the row's code,
+ * store() writes beside the codes. */
+template <int T, int V, typename OP>
+__global__ void __launch_bounds__(T < 256 ? 256 : T) k_rows(OP op, uint64_t rows, uint32_t cols)
+{
+    constexpr int B = T < 256 ? 256 : T, R = B / T, W = T / 64, N = V ? V : 1;
+    __shared__ uint32_t part[2][2][W > 1 ? W : 1];
+    const uint32_t t = threadIdx.x % T;
+    uint32_t turn = 0;
+    for (uint64_t row = (uint64_t)blockIdx.x * R + threadIdx.x / T; row < rows; row += (uint64_t)gridDim.x * R, turn ^= 1u) {
+        typename OP::Reg reg[N];
+        uint32_t m = 0;
+        float sum = 0.0f;
+        auto at = [&](uint32_t i) { return (i * T + t) * 8u; };
+        auto left = [&](uint32_t c) { return c < cols ? (int)min(cols - c, 8u) : 0; };
+        const uint32_t steps = V ? V : (cols + T * 8u - 1u) / (T * 8u);
+        if (V) {
+#pragma unroll
+            for (int i = 0; i < N; i++) op.load(row, at(i), left(at(i)), reg[i], m, sum, true);
+        } else {
+            for (uint32_t i = 0; i < steps; i++) op.load(row, at(i), left(at(i)), reg[0], m, sum, true);
+        }
+        m = wave_all(m, max_of);
+        if (OP::SUMS) sum = from_bits(wave_all(to_bits(sum), sum_of));
+        if (W > 1) {
+            if (threadIdx.x % 64 == 0) {
+                part[turn][0][threadIdx.x / 64] = m;
+                if (OP::SUMS) part[turn][1][threadIdx.x / 64] = to_bits(sum);
+            }
+            wg_sync();                       /* the other half of `part` is this one's past: one barrier per row does */
+            m = 0;
+            sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < W; i++) {
+                m = max(m, part[turn][0][i]);
+                if (OP::SUMS) sum += from_bits(part[turn][1][i]);
+            }
+        }
+        const RowCode rc = row_code(m);
+        op.done(row, t == 0, sum, rc, cols);
+        if (V) {
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                const uint32_t c = at(i);
+                if (c < cols) *reinterpret_cast<uint2 *>(op.q.at(row, c)) = row_codes8(reg[i].t, rc.inv);
+                op.store(row, c, cols, reg[i]);
+            }
+        } else {
+            for (uint32_t i = 0; i < steps; i++) {
+                const uint32_t c = at(i);
+                uint32_t m2 = 0;
+                float s2 = 0.0f;
+                op.load(row, c, left(c), reg[0], m2, s2, false);
+                if (c < cols) *reinterpret_cast<uint2 *>(op.q.at(row, c)) = row_codes8(reg[0].t, rc.inv);
+                op.store(row, c, cols, reg[0]);
+            }
+        }
+    }
+}
+
+template <int T, int V, typename OP> int go_rows(const OP &op, uint64_t rows, uint32_t cols, hipStream_t st)
+{
+    constexpr uint64_t R = T < 256 ? 256 / T : 1;
+    const uint64_t blocks = (rows + R - 1) / R;
+    k_rows<T, V, OP><<<(uint32_t)(blocks < (1u << 20) ? blocks : 1u << 20), T < 256 ? 256 : T, 0, st>>>(op, rows, cols);
+    return launched();
+}
+/* A wavefront holds rows of up to 1024 columns, four wavefronts up to 8192, sixteen up to 32768. */
+template <typename OP> int launch_rows(const OP &op, uint64_t rows, uint32_t cols, hipStream_t st)
+{
+    if (rows == 0) return NSML_OK;
+    if (cols <= 512) return go_rows<64, 1>(op, rows, cols, st);
+    if (cols <= 1024) return go_rows<64, 2>(op, rows, cols, st);
+    if (cols <= 2048) return go_rows<256, 1>(op, rows, cols, st);
+    if (cols <= 4096) return go_rows<256, 2>(op, rows, cols, st);
+    if (cols <= 8192) return go_rows<256, 4>(op, rows, cols, st);
+    if (cols <= 16384) return go_rows<1024, 2>(op, rows, cols, st);
+    if (cols <= 32768) return go_rows<1024, 4>(op, rows, cols, st);
+    return go_rows<1024, 0>(op, rows, cols, st);
+}
+
+template <typename T> struct OpRows {
+    static constexpr bool SUMS = false;
+    struct Reg { float t[8]; };
+    Mat<const T> x;
+    const float *col;
+    Mat<int8_t> q;
+    float *scale;
+    __device__ __forceinline__ void load(uint64_t row, uint32_t c, int n, Reg &r, uint32_t &m, float &, bool) const
+    {
+        load8(x.at(row, c), n, r.t);
+        if (col) {
+            float f[8];
+            load8(col + c, n, f);
+#pragma unroll
+            for (int i = 0; i < 8; i++) r.t[i] *= f[i];
+        }
+        m = max8(r.t, m);
+    }
+    __device__ __forceinline__ void done(uint64_t row, bool first, float, RowCode rc, uint32_t) const
+    {
+        if (first) scale[row] = rc.scale;
+    }
+    __device__ __forceinline__ void store(uint64_t, uint32_t, uint32_t, const Reg &) const {}
+};
+
+/* The norm: codes are those of gamma * h, so that they wait for the absmax alone; the mean of h^2, which comes out of
+ * the same reduction, goes into the scale. */
+template <typename T> struct OpNorm {
+    static constexpr bool SUMS = true;
+    struct Reg { float t[8], h[8]; };
+    Mat<const T> x, res;
+    const float *gamma;
+    float eps;
+    Mat<T> h;
+    Mat<int8_t> q;
+    float *scale, *rstd;
+    Ckpt xhat;
+    float r = 0.0f;                          /* the row's 1 / rms */
+    __device__ __forceinline__ void load(uint64_t row, uint32_t c, int n, Reg &g, uint32_t &m, float &sum, bool first) const
+    {
+        load8(x.at(row, c), n, g.h);
+        if (res.p) {
+            float f[8];
+            load8(res.at(row, c), n, f);
+#pragma unroll
+            for (int i = 0; i < 8; i++) g.h[i] = (float)(T)(g.h[i] + f[i]);
+            if (first && n) store8(h.at(row, c), n, g.h);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            sum = __builtin_fmaf(g.h[i], g.h[i], sum);
+            g.t[i] = g.h[i];
+        }
+        if (gamma) {
+            float f[8];
+            load8(gamma + c, n, f);
+#pragma unroll
+            for (int i = 0; i < 8; i++) g.t[i] *= f[i];
+        }
+        m = max8(g.t, m);
+    }
+    __device__ __forceinline__ void done(uint64_t row, bool first, float sum, RowCode rc, uint32_t cols)
+    {
+        r = rsqrtf(sum / (float)cols + eps);
+        if (first) {
+            rstd[row] = r;
+            scale[row] = rc.scale * r;
+        }
+    }
+    __device__ __forceinline__ void store(uint64_t row, uint32_t c, uint32_t cols, const Reg &g) const
+    {
+        if (!xhat.q) return;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = g.h[i] * r;
+        ckpt_store8(xhat, row, c, cols, v);
+    }
+};
+
+/* 1 / (1 + exp(-x)) by the GPU's exponential of two and reciprocal: under 2 units in the last place for |x| < 20, 0 and 1 at
+ * the infinities. */
+__device__ __forceinline__ float sigmoid(float x)
+{
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -1.44269504f));
+}
+
+template <typename T> struct OpGlu {
+    static constexpr bool SUMS = false;
+    struct Reg { float t[8]; };
+    Mat<const T> gate, up;
+    Mat<int8_t> q;
+    float *scale;
+    Ckpt kg, ku, ka;
+    uint32_t cols;
+    __device__ __forceinline__ void load(uint64_t row, uint32_t c, int n, Reg &r, uint32_t &m, float &, bool first) const
+    {
+        float g[8], u[8];
+        load8(gate.at(row, c), n, g);
+        load8(up.at(row, c), n, u);
+        if (first && kg.q) ckpt_store8(kg, row, c, cols, g);
+        if (first && ku.q) ckpt_store8(ku, row, c, cols, u);
+#pragma unroll
+        for (int i = 0; i < 8; i++) r.t[i] = g[i] * sigmoid(g[i]) * u[i];
+        m = max8(r.t, m);
+    }
+    __device__ __forceinline__ void done(uint64_t row, bool first, float, RowCode rc, uint32_t) const
+    {
+        if (first) scale[row] = rc.scale;
+    }
+    __device__ __forceinline__ void store(uint64_t row, uint32_t c, uint32_t n, const Reg &r) const
+    {
+        if (ka.q) ckpt_store8(ka, row, c, n, r.t);
+    }
+};
+
+/* ---------------------------------------------------------------- elements and blocks */
+
+/* Eight neighbours per thread, L threads side by side in a row, 256 / L rows per workgroup; workgroups side by side cover
+ * a window that moves through memory. */
+template <typename OP> __global__ void __launch_bounds__(256) k_each(OP op, uint64_t rows, uint32_t cols, uint32_t log2l)
+{
+    const uint32_t c = ((blockIdx.x << log2l) + (threadIdx.x & ((1u << log2l) - 1u))) * 8u;
+    const uint32_t per = 256u >> log2l;
+    const int n = c < cols ? (int)min(cols - c, 8u) : 0;
+    for (uint64_t row = (uint64_t)blockIdx.y * per + (threadIdx.x >> log2l); row < rows; row += (uint64_t)gridDim.y * per)
+        op.run(row, c, n, cols);
+}
+template <typename OP> int launch_each(const OP &op, uint64_t rows, uint32_t cols, hipStream_t st)
+{
+    if (rows == 0) return NSML_OK;
+    const uint32_t vecs = (cols + 31u) / 32u * 4u;
+    uint32_t log2l = 2;
+    while (log2l < 8u && (1u << log2l) < vecs) log2l++;
+    const uint64_t groups = (rows + (256u >> log2l) - 1) / (256u >> log2l);
+    k_each<OP><<<dim3((vecs + (1u << log2l) - 1u) >> log2l, (uint32_t)(groups < 65535u ? groups : 65535u)), 256, 0, st>>>(op, rows, cols, log2l);
+    return launched();
+}
+
+template <typename T> struct OpPack {
+    Mat<const T> x;
+    Ckpt k;
+    __device__ __forceinline__ void run(uint64_t row, uint32_t c, int n, uint32_t cols) const
+    {
+        float v[8];
+        load8(x.at(row, c), n, v);
+        ckpt_store8(k, row, c, cols, v);
+    }
+};
+template <typename T> struct OpUnpack {
+    Ckpt k;
+    Mat<T> out;
+    __device__ __forceinline__ void run(uint64_t row, uint32_t c, int n, uint32_t) const
+    {
+        if (!n) return;
+        float v[8];
+        ckpt_load8(k, row, c, v);
+        store8(out.at(row, c), n, v);
+    }
+};
+template <typename T> struct OpValues {
+    Mat<const int8_t> q;
+    const float *scale;
+    Mat<T> out;
+    __device__ __forceinline__ void run(uint64_t row, uint32_t c, int n, uint32_t) const
+    {
+        if (!n) return;
+        float v[8];
+        codes8(*reinterpret_cast<const uint2 *>(q.at(row, c)), v);
+        const float s = scale ? scale[row] : 1.0f;
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] *= s;
+        store8(out.at(row, c), n, v);
+    }
+};
+template <typename T> struct OpGluBack {
+    Mat<const T> da;
+    Ckpt kg, ku;
+    Mat<T> dg, du;
+    __device__ __forceinline__ void run(uint64_t row, uint32_t c, int n, uint32_t) const
+    {
+        if (!n) return;
+        float a[8], g[8], u[8];
+        load8(da.at(row, c), n, a);
+        ckpt_load8(kg, row, c, g);
+        ckpt_load8(ku, row, c, u);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float s = sigmoid(g[i]), d = a[i] * s;
+            u[i] = d * u[i] * __builtin_fmaf(g[i], 1.0f - s, 1.0f);
+            a[i] = d * g[i];
+        }
+        store8(dg.at(row, c), n, u);
+        store8(du.at(row, c), n, a);
+    }
+};
+
+/* ---------------------------------------------------------------- gradient of the norm */
+
+/* T threads hold a row; a workgroup takes every so many rows and keeps its share of dgamma in registers, one row of
+ * `part` for each T threads at the end, which k_norm_sum adds up in order. */
+template <typename X, int T, int V>
+__global__ void __launch_bounds__(T < 256 ? 256 : T)
+k_norm_back(Mat<const X> dy, Ckpt xhat, const float *rstd, const float *gamma, Mat<const X> dres, Mat<X> dx, float *part,
+            uint64_t rows, uint32_t cols)
+{
+    constexpr int B = T < 256 ? 256 : T, R = B / T, W = T / 64;
+    __shared__ uint32_t sums[2][W > 1 ? W : 1];
+    const uint32_t t = threadIdx.x % T;
+    const uint64_t first = (uint64_t)blockIdx.x * R + threadIdx.x / T, step = (uint64_t)gridDim.x * R;
+    float g[V][8], dg[V][8];
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+        const uint32_t c = (i * T + t) * 8u;
+#pragma unroll
+        for (int j = 0; j < 8; j++) g[i][j] = 1.0f, dg[i][j] = 0.0f;
+        if (gamma && c < cols) load8(gamma + c, (int)min(cols - c, 8u), g[i]);
+    }
+    uint32_t turn = 0;
+    for (uint64_t row = first; row < rows; row += step, turn ^= 1u) {
+        float d[V][8], x[V][8];
+        float dot = 0.0f;
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            const uint32_t c = (i * T + t) * 8u;
+            if (c < cols) {
+                load8(dy.at(row, c), (int)min(cols - c, 8u), d[i]);
+                ckpt_load8(xhat, row, c, x[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            const uint32_t c = (i * T + t) * 8u;
+            if (c < cols) {
+#pragma unroll
+                for (int j = 0; j < 8; j++) {
+                    if (c + j >= cols) x[i][j] = 0.0f;      /* codes beyond the row are not values */
+                    dg[i][j] = __builtin_fmaf(d[i][j], x[i][j], dg[i][j]);
+                    d[i][j] *= g[i][j];
+                    dot = __builtin_fmaf(d[i][j], x[i][j], dot);
+                }
+            }
+        }
+        dot = from_bits(wave_all(to_bits(dot), sum_of));
+        if (W > 1) {
+            if (threadIdx.x % 64 == 0) sums[turn][threadIdx.x / 64] = to_bits(dot);
+            wg_sync();
+            dot = 0.0f;
+#pragma unroll
+            for (int i = 0; i < W; i++) dot += from_bits(sums[turn][i]);
+        }
+        const float mean = dot / (float)cols, r = rstd[row];
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            const uint32_t c = (i * T + t) * 8u;
+            if (c < cols) {
+                const int n = (int)min(cols - c, 8u);
+                float v[8] = {};
+                if (dres.p) load8(dres.at(row, c), n, v);
+#pragma unroll
+                for (int j = 0; j < 8; j++) v[j] = __builtin_fmaf(r, d[i][j] - x[i][j] * mean, v[j]);
+                store8(dx.at(row, c), n, v);
+            }
+        }
+    }
+    if (!part || first >= rows) return;
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+        const uint32_t c = (i * T + t) * 8u;
+        if (c < cols) store8(part + first * cols + c, (int)min(cols - c, 8u), dg[i]);
+    }
+}
+
+/* dgamma[i] = sum of part[0..groups)[i]: 16 columns (a 64-byte line) by 64 slices per workgroup, the slices added in order. */
+__global__ void __launch_bounds__(1024) k_norm_sum(const float *part, uint32_t groups, uint32_t cols, float *dgamma)
+{
+    __shared__ float s[64][17];
+    const uint32_t lane = threadIdx.x % 16, slice = threadIdx.x / 16, c = blockIdx.x * 16u + lane;
+    float sum = 0.0f;
+    if (c < cols)
+        for (uint32_t g = slice; g < groups; g += 64) sum += part[(uint64_t)g * cols + c];
+    s[slice][lane] = sum;
+    wg_sync();
+    if (threadIdx.x < 16 && c < cols) {
+        sum = 0.0f;
+        for (int i = 0; i < 64; i++) sum += s[i][lane];
+        dgamma[c] = sum;
+    }
+}
+
+/* Threads per row, and how many rows are worked on at the same time (each leaves a row of partial sums). */
+struct BackShape { uint32_t threads, groups; };
+BackShape back_shape(uint64_t rows, uint32_t cols)
+{
+    const uint32_t threads = cols <= 1024 ? 64 : cols <= 8192 ? 256 : 1024;
+    const uint32_t most = threads == 64 ? 2048u : threads == 256 ? 512u : 256u;
+    return {threads, (uint32_t)(rows < most ? rows : most)};
+}
+
+template <typename X, int T, int V, typename... A>
+int go_back(uint32_t groups, hipStream_t st, A... a)
+{
+    constexpr uint32_t R = T < 256 ? 256 / T : 1;
+    k_norm_back<X, T, V><<<(groups + R - 1) / R, T < 256 ? 256 : T, 0, st>>>(a...);
+    return launched();
+}
+template <typename X, typename... A> int launch_back(uint32_t cols, uint32_t groups, hipStream_t st, A... a)
+{
+    if (cols <= 512) return go_back<X, 64, 1>(groups, st, a...);
+    if (cols <= 1024) return go_back<X, 64, 2>(groups, st, a...);
+    if (cols <= 2048) return go_back<X, 256, 1>(groups, st, a...);
+    if (cols <= 4096) return go_back<X, 256, 2>(groups, st, a...);
+    if (cols <= 8192) return go_back<X, 256, 4>(groups, st, a...);
+    if (cols <= 16384) return go_back<X, 1024, 2>(groups, st, a...);
+    return go_back<X, 1024, 4>(groups, st, a...);
+}
+
+template <typename F> int by_type(int type, F f)
+{
+    if (type == NSML_F32) return f(float{});
+    if (type == NSML_BF16) return f(bf16{});
+    return f(f16{});
+}
+
+}  // namespace
+
+extern "C" {
+
+int nsml_q8_rows(const void *x, int type, uint64_t ldx, uint64_t rows, uint32_t cols, const float *col_scale,
+                 int8_t *q, uint64_t ldq, float *scale, void *stream)
+{
+    if (cols == 0 || bad_type(type) || (col_scale && bad_f32(col_scale)) ||
+        (rows && (bad_mat(x, type, ldx, cols) || bad_codes(q, ldq, cols) || bad_f32(scale))))
+        return NSML_EINVAL;
+    if (cols > NSML_Q8_MAX_COLS) return NSML_ECAP;
+    return by_type(type, [&](auto v) {
+        using T = decltype(v);
+        return launch_rows(OpRows<T>{mat<T>(x, ldx), col_scale, mat<int8_t>((void *)q, ldq), scale}, rows, cols, (hipStream_t)stream);
+    });
+}
+
+int nsml_q8_values(const int8_t *q, uint64_t ldq, const float *scale, uint64_t rows, uint32_t cols,
+                   void *out, int type, uint64_t ldo, void *stream)
+{
+    if (cols == 0 || bad_type(type) || (rows && (bad_codes(q, ldq, cols) || (scale && bad_f32(scale)) || bad_mat(out, type, ldo, cols))))
+        return NSML_EINVAL;
+    return by_type(type, [&](auto v) {
+        using T = decltype(v);
+        return launch_each(OpValues<T>{mat<int8_t>((const void *)q, ldq), scale, mat<T>(out, ldo)}, rows, cols, (hipStream_t)stream);
+    });
+}
+
+int nsml_ckpt8_pack(const void *x, int type, uint64_t ldx, uint64_t rows, uint32_t cols, const nsml_ckpt8 *out, void *stream)
+{
+    if (cols == 0 || bad_type(type) || (rows && (bad_mat(x, type, ldx, cols) || bad_ckpt(out, cols)))) return NSML_EINVAL;
+    return by_type(type, [&](auto v) {
+        using T = decltype(v);
+        return launch_each(OpPack<T>{mat<T>(x, ldx), ckpt_of(out)}, rows, cols, (hipStream_t)stream);
+    });
+}
+
+int nsml_ckpt8_unpack(const nsml_ckpt8 *x, uint64_t rows, uint32_t cols, void *out, int type, uint64_t ldo, void *stream)
+{
+    if (cols == 0 || bad_type(type) || (rows && (bad_ckpt(x, cols) || bad_mat(out, type, ldo, cols)))) return NSML_EINVAL;
+    return by_type(type, [&](auto v) {
+        using T = decltype(v);
+        return launch_each(OpUnpack<T>{ckpt_of(x), mat<T>(out, ldo)}, rows, cols, (hipStream_t)stream);
+    });
+}
+
+int nsml_rmsnorm_q8(const void *x, uint64_t ldx, const void *residual, uint64_t ldr, const float *gamma, float eps,
+                    int type, uint64_t rows, uint32_t cols, void *h, uint64_t ldh, int8_t *q, uint64_t ldq,
+                    float *scale, float *rstd, const nsml_ckpt8 *xhat, void *stream)
+{
+    if (cols == 0 || bad_type(type) || !(eps >= 0.0f) || (gamma && bad_f32(gamma)) ||
+        (rows && (bad_mat(x, type, ldx, cols) || !residual != !h ||
+                  (residual && (bad_mat(residual, type, ldr, cols) || bad_mat(h, type, ldh, cols))) ||
+                  bad_codes(q, ldq, cols) || bad_f32(scale) || bad_f32(rstd) || (xhat && bad_ckpt(xhat, cols)))))
+        return NSML_EINVAL;
+    if (cols > NSML_NORM_MAX_COLS) return NSML_ECAP;
+    return by_type(type, [&](auto v) {
+        using T = decltype(v);
+        return launch_rows(OpNorm<T>{mat<T>(x, ldx), mat<T>(residual, ldr), gamma, eps, mat<T>(h, ldh),
+                                     mat<int8_t>((void *)q, ldq), scale, rstd, ckpt_of(xhat)}, rows, cols, (hipStream_t)stream);
+    });
+}
+
+uint64_t nsml_rmsnorm_backward_work(uint64_t rows, uint32_t cols)
+{
+    return (uint64_t)back_shape(rows, cols).groups * cols * 4u;
+}
+
+int nsml_rmsnorm_backward(const void *dy, uint64_t lddy, const nsml_ckpt8 *xhat, const float *rstd, const float *gamma,
+                          const void *dres, uint64_t lddres, int type, uint64_t rows, uint32_t cols,
+                          void *dx, uint64_t lddx, float *dgamma, void *work, uint64_t work_bytes, void *stream)
+{
+    if (cols == 0 || bad_type(type) || (gamma && bad_f32(gamma)) ||
+        (rows && (bad_mat(dy, type, lddy, cols) || bad_ckpt(xhat, cols) || bad_f32(rstd) ||
+                  (dres && bad_mat(dres, type, lddres, cols)) || bad_mat(dx, type, lddx, cols))))
+        return NSML_EINVAL;
+    if (cols > NSML_NORM_MAX_COLS) return NSML_ECAP;
+    const BackShape s = back_shape(rows, cols);
+    float *part = nullptr;
+    if (dgamma) {
+        if (bad_f32(dgamma)) return NSML_EINVAL;
+        if (rows && (!work || !at_multiple(work, 16) || work_bytes < nsml_rmsnorm_backward_work(rows, cols))) return NSML_EINVAL;
+        part = static_cast<float *>(work);
+    }
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (rows) {
+        const int rc = by_type(type, [&](auto v) {
+            using T = decltype(v);
+            return launch_back<T>(cols, s.groups, st, mat<T>(dy, lddy), ckpt_of(xhat), rstd, gamma, mat<T>(dres, lddres),
+                                  mat<T>(dx, lddx), part, rows, cols);
+        });
+        if (rc) return rc;
+    }
+    if (dgamma) {
+        k_norm_sum<<<(cols + 15u) / 16u, 1024, 0, st>>>(part, s.groups, cols, dgamma);
+        return launched();
+    }
+    return NSML_OK;
+}
+
+int nsml_swiglu_q8(const void *gate, uint64_t ldg, const void *up, uint64_t ldu, int type, uint64_t rows, uint32_t cols,
+                   int8_t *q, uint64_t ldq, float *scale, const nsml_ckpt8 *gate_ckpt, const nsml_ckpt8 *up_ckpt,
+                   const nsml_ckpt8 *act_ckpt, void *stream)
+{
+    if (cols == 0 || bad_type(type) ||
+        (rows && (bad_mat(gate, type, ldg, cols) || bad_mat(up, type, ldu, cols) || bad_codes(q, ldq, cols) || bad_f32(scale) ||
+                  (gate_ckpt && bad_ckpt(gate_ckpt, cols)) || (up_ckpt && bad_ckpt(up_ckpt, cols)) || (act_ckpt && bad_ckpt(act_ckpt, cols)))))
+        return NSML_EINVAL;
+    if (cols > NSML_Q8_MAX_COLS) return NSML_ECAP;
+    return by_type(type, [&](auto v) {
+        using T = decltype(v);
+        return launch_rows(OpGlu<T>{mat<T>(gate, ldg), mat<T>(up, ldu), mat<int8_t>((void *)q, ldq), scale, ckpt_of(gate_ckpt),
+                                    ckpt_of(up_ckpt), ckpt_of(act_ckpt), cols}, rows, cols, (hipStream_t)stream);
+    });
+}
+
+int nsml_swiglu_backward(const void *da, uint64_t ldda, const nsml_ckpt8 *gate, const nsml_ckpt8 *up, int type,
+                         uint64_t rows, uint32_t cols, void *dgate, uint64_t lddg, void *dup, uint64_t lddu, void *stream)
+{
+    if (cols == 0 || bad_type(type) ||
+        (rows && (bad_mat(da, type, ldda, cols) || bad_ckpt(gate, cols) || bad_ckpt(up, cols) ||
+                  bad_mat(dgate, type, lddg, cols) || bad_mat(dup, type, lddu, cols))))
+        return NSML_EINVAL;
+    return by_type(type, [&](auto v) {
+        using T = decltype(v);
+        return launch_each(OpGluBack<T>{mat<T>(da, ldda), ckpt_of(gate), ckpt_of(up), mat<T>(dgate, lddg), mat<T>(dup, lddu)}, rows, cols,
+                           (hipStream_t)stream);
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,166 @@
+"""What the 8-bit layer's entry points and their binding refuse, before any kernel is launched (no GPU needed: the library's own
+checks come before its first HIP call, and CPU tensors stand in for device tensors in the binding's)."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2506_16235_amd import binding as nsml
+
+L = nsml.raw()
+P = 1 << 12                 # an address that is aligned to everything; nothing is read from it
+
+
+def ck(q=P, e=P, ldq=64, lde=2):
+    return C.byref(nsml._CkptArg(q, e, ldq, lde))
+
+
+def refused(rc, code=None):
+    assert rc == (nsml.EINVAL if code is None else code)
+
+
+def test_rows_and_values():
+    def rows(x=P, type=0, ldx=64, m=3, k=64, col=None, q=P, ldq=64, s=P):
+        return L.nsml_q8_rows(x, type, ldx, m, k, col, q, ldq, s, None)
+    for bad in ({"x": None}, {"x": P + 2}, {"type": 3}, {"type": -1}, {"ldx": 63}, {"k": 0}, {"col": P + 1}, {"q": None}, {"q": P + 8},
+                {"ldq": 72}, {"ldq": 48}, {"s": None}, {"s": P + 2}):
+        refused(rows(**bad))
+    refused(rows(k=131073, ldx=1 << 20, ldq=1 << 20), nsml.ECAP)
+
+    def values(q=P, ldq=64, s=P, m=3, k=64, out=P, type=1, ldo=64):
+        return L.nsml_q8_values(q, ldq, s, m, k, out, type, ldo, None)
+    for bad in ({"q": None}, {"ldq": 65}, {"s": P + 1}, {"k": 0}, {"out": None}, {"out": P + 1}, {"type": 9}, {"ldo": 10}):
+        refused(values(**bad))
+
+
+def test_matmul():
+    def mm(a=P, lda=64, sa=P, b=P, ldb=64, sb=P, bias=None, m=3, n=5, k=64, c=P, type=1, ldc=5):
+        return L.nsml_q8_matmul(a, lda, sa, b, ldb, sb, bias, m, n, k, c, type, ldc, None)
+    for bad in ({"a": None}, {"a": P + 4}, {"lda": 60}, {"sa": None}, {"b": None}, {"ldb": 63}, {"sb": P + 2}, {"bias": P + 3}, {"n": 0},
+                {"k": 0}, {"c": None}, {"c": P + 1}, {"type": 5}, {"ldc": 4}):
+        refused(mm(**bad))
+    refused(mm(k=131088, lda=131088, ldb=131088), nsml.ECAP)
+    refused(mm(lda=(1 << 22) + 16), nsml.ECAP)
+
+
+def test_checkpoints():
+    for bad in (ck(q=None), ck(q=P + 8), ck(e=None), ck(ldq=72), ck(ldq=48), ck(lde=1), None):
+        refused(L.nsml_ckpt8_pack(P, 0, 64, 3, 64, bad, None))
+        refused(L.nsml_ckpt8_unpack(bad, 3, 64, P, 0, 64, None))
+        refused(L.nsml_ckpt8_wgrad(P, 0, 8, bad, None, 3, 8, 64, None, P, 64, None, 0, None))
+        refused(L.nsml_rmsnorm_backward(P, 64, bad, P, None, None, 0, 0, 3, 64, P, 64, None, None, 0, None))
+        refused(L.nsml_swiglu_backward(P, 64, bad, ck(), 0, 3, 64, P, 64, P, 64, None))
+        refused(L.nsml_swiglu_backward(P, 64, ck(), bad, 0, 3, 64, P, 64, P, 64, None))
+        if bad is not None:
+            refused(L.nsml_rmsnorm_q8(P, 64, None, 0, None, 0.0, 0, 3, 64, None, 0, P, 64, P, P, bad, None))
+            refused(L.nsml_swiglu_q8(P, 64, P, 64, 0, 3, 64, P, 64, P, bad, None, None, None))
+    refused(L.nsml_ckpt8_pack(P, 7, 64, 3, 64, ck(), None))
+    refused(L.nsml_ckpt8_pack(P + 1, 1, 64, 3, 64, ck(), None))
+    refused(L.nsml_ckpt8_unpack(ck(), 3, 0, P, 0, 64, None))
+
+
+def test_wgrad():
+    def wg(dy=P, type=1, lddy=1000, col=None, m=4000, n=1000, k=64, add=None, dw=P, ld=64, work=P, size=1 << 40):
+        return L.nsml_ckpt8_wgrad(dy, type, lddy, ck(), col, m, n, k, add, dw, ld, work, size, None)
+    for bad in ({"dy": None}, {"dy": P + 1}, {"type": 4}, {"lddy": 999}, {"col": P + 2}, {"n": 0}, {"k": 0}, {"add": P + 1}, {"dw": None},
+                {"ld": 63}, {"work": None}, {"work": P + 8}, {"size": L.nsml_ckpt8_wgrad_work(4000, 1000, 64) - 1}):
+        refused(wg(**bad))
+    assert L.nsml_ckpt8_wgrad_work(4000, 1000, 64) > 0 and L.nsml_ckpt8_wgrad_work(0, 1000, 64) == 0
+
+
+def test_norm():
+    def nq(x=P, ldx=64, r=None, ldr=0, g=None, eps=1e-5, type=0, m=3, k=64, h=None, ldh=0, q=P, ldq=64, s=P, rstd=P):
+        return L.nsml_rmsnorm_q8(x, ldx, r, ldr, g, eps, type, m, k, h, ldh, q, ldq, s, rstd, None, None)
+    for bad in ({"x": None}, {"ldx": 3}, {"r": P, "ldr": 64}, {"h": P, "ldh": 64}, {"r": P, "ldr": 63, "h": P, "ldh": 64},
+                {"r": P, "ldr": 64, "h": P, "ldh": 63}, {"g": P + 2}, {"eps": -1.0}, {"eps": float("nan")}, {"type": 3}, {"k": 0}, {"q": None},
+                {"ldq": 16}, {"s": None}, {"rstd": None}):
+        refused(nq(**bad))
+    refused(nq(k=32769, ldx=40000, ldq=40000), nsml.ECAP)
+
+    def nb(dy=P, ld=64, rstd=P, g=None, dres=None, ldr=0, type=0, k=64, dx=P, ldx=64, dg=P, work=P, size=1 << 40):
+        return L.nsml_rmsnorm_backward(dy, ld, ck(), rstd, g, dres, ldr, type, 3, k, dx, ldx, dg, work, size, None)
+    for bad in ({"dy": None}, {"ld": 1}, {"rstd": None}, {"g": P + 1}, {"dres": P, "ldr": 60}, {"type": 8}, {"k": 0}, {"dx": None},
+                {"ldx": 2}, {"dg": P + 2}, {"work": None}, {"work": P + 4}, {"size": L.nsml_rmsnorm_backward_work(3, 64) - 1}):
+        refused(nb(**bad))
+
+
+def test_swiglu():
+    def sg(g=P, ldg=64, u=P, ldu=64, type=0, k=64, q=P, ldq=64, s=P):
+        return L.nsml_swiglu_q8(g, ldg, u, ldu, type, 3, k, q, ldq, s, None, None, None, None)
+    for bad in ({"g": None}, {"ldg": 63}, {"u": None}, {"u": P + 2}, {"ldu": 1}, {"type": 3}, {"k": 0}, {"q": P + 1}, {"ldq": 68}, {"s": None}):
+        refused(sg(**bad))
+    for bad in ({"da": None}, {"dg": None}, {"du": P + 2}, {"ld": 63}):
+        a = {"da": P, "dg": P, "du": P, "ld": 64, **bad}
+        refused(L.nsml_swiglu_backward(a["da"], a["ld"], ck(), ck(), 0, 3, 64, a["dg"], 64, a["du"], 64, None))
+
+
+# ---------------------------------------------------------------- the binding's own checks
+
+CPU = torch.device("cpu")
+
+
+def test_binding_wants_tensors_on_a_gpu():
+    x = torch.zeros(4, 32)
+    q = nsml.Q8(torch.zeros(4, 32, dtype=torch.int8), torch.ones(4))
+    c = nsml.Ckpt8(torch.zeros(4, 32, dtype=torch.int8), torch.zeros(4, 1, dtype=torch.uint8))
+    for call in (lambda: nsml.q8_rows(x), lambda: nsml.q8_values(q), lambda: nsml.q8_matmul(q, q), lambda: nsml.ckpt8_pack(x),
+                 lambda: nsml.ckpt8_unpack(c), lambda: nsml.ckpt8_wgrad(x, c), lambda: nsml.rmsnorm_q8(x),
+                 lambda: nsml.rmsnorm_backward(x, c, torch.ones(4)), lambda: nsml.swiglu_q8(x, x),
+                 lambda: nsml.swiglu_backward(x, c, c), lambda: nsml.q8_rows(None)):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_binding_checks_matrices():
+    ok = torch.zeros(4, 40)
+    assert nsml._matrix("x", ok, CPU)[1:] == (40, 4, 40)
+    assert nsml._matrix("x", ok[:, :30], CPU)[1:] == (40, 4, 30)
+    assert nsml._matrix("x", ok[:1, :30], CPU)[1] >= 30
+    for bad, kw in ((ok.t(), {}), (ok[0], {}), (ok.double(), {}), (ok.half(), {"dtype": torch.float32}), (ok, {"rows": 5}), (ok, {"cols": 39}),
+                    (ok[:, :0], {}), (ok[:, ::2], {}), (ok[:1].expand(4, 40), {}), ([1, 2], {}), (torch.zeros(2, 2, 2), {})):
+        with pytest.raises(ValueError):
+            nsml._matrix("x", bad, CPU, kw.get("dtype"), kw.get("rows"), kw.get("cols"))
+    with pytest.raises(ValueError):
+        nsml._matrix("x", ok, torch.device("cuda", 0))
+
+
+def _aligned(*shape):
+    n = 1
+    for s in shape:
+        n *= s
+    flat = torch.zeros(n + 16, dtype=torch.int8)
+    lead = -flat.data_ptr() % 16
+    return flat[lead:lead + n].view(shape), flat, lead
+
+
+def test_binding_checks_codes():
+    q, flat, lead = _aligned(4, 48)
+    assert nsml._codes("q", q, CPU)[1:] == (48, 4, 48)
+    assert nsml._codes("q", q[:, :40], CPU)[1:] == (48, 4, 40)
+    with pytest.raises(ValueError):
+        nsml._codes("q", q[:, 1:41], CPU)                                   # does not start at a multiple of 16
+    with pytest.raises(ValueError):
+        nsml._codes("q", torch.zeros(4, 40, dtype=torch.int8), CPU)         # stride 40
+    with pytest.raises(ValueError):
+        nsml._codes("q", q.to(torch.uint8), CPU)
+    short = torch.zeros(lead + 3 * 48 + 40 + 16, dtype=torch.int8)
+    lead = -short.data_ptr() % 16
+    short = torch.empty(0, dtype=torch.int8).set_(short.untyped_storage()[:lead + 3 * 48 + 40], lead, (4, 40), (48, 1))
+    with pytest.raises(ValueError):
+        nsml._codes("q", short, CPU)                                        # the last row's 16-byte chunk is not its own
+
+
+def test_binding_checks_vectors_and_pairs():
+    assert nsml._vector("v", None, CPU, 5) is None
+    for bad in (torch.zeros(4), torch.zeros(5, dtype=torch.float64), torch.zeros(10)[::2], torch.zeros(5, 1), 3.0):
+        with pytest.raises(ValueError):
+            nsml._vector("v", bad, CPU, 5)
+    q, _, _ = _aligned(4, 48)
+    with pytest.raises(ValueError):
+        nsml._rows_of("a", (q, torch.ones(4)), CPU)
+    with pytest.raises(ValueError):
+        nsml._rows_of("a", nsml.Q8(q, torch.ones(3)), CPU)
+    with pytest.raises(ValueError):
+        nsml._ckpt("c", nsml.Ckpt8(q, torch.zeros(4, 1, dtype=torch.uint8)), CPU)       # needs two exponents a row
+    with pytest.raises(ValueError):
+        nsml._ckpt("c", nsml.Q8(q, torch.ones(4)), CPU)
