@@ -24,7 +24,9 @@ template <typename T> struct Out {
 
 /* ---------------------------------------------------------------- tiles */
 
-/* A tile of BM x BN by WM x WN wavefronts; k in stages of 128 bytes, loaded straight into LDS one stage ahead. */
+/* A tile of BM x BN by WM x WN wavefronts; k in stages of 128 bytes, loaded straight into LDS one stage ahead.
+ * The matrix instructions of the last quarter of a stage run while the first quarter of the next is read from LDS: the barrier
+ * between stages stands before them, when all of the stage is in registers. */
 template <typename T, int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(WM * WN * 64)
 k_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t m, uint32_t n, uint32_t k, Out<T> out)
@@ -39,6 +41,7 @@ k_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t
     const uint32_t rows_a = (uint32_t)min<uint64_t>(m - m0, BM), rows_b = min(n - n0, (uint32_t)BN);
     const uint32_t wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
     v16i acc[TM][TN] = {};
+    v4i fa[2][TM], fb[2][TN];
     const int8_t *pa = a + m0 * lda, *pb = b + (uint64_t)n0 * ldb;
     auto fetch = [&](uint32_t k0, uint8_t *to) {
         if (k - k0 >= 128u) {
@@ -49,42 +52,83 @@ k_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t
             load_tail<BN, W>(pb + k0, ldb, rows_b, k - k0, to + BM * 128, threadIdx.x);
         }
     };
-    auto step = [&](const uint8_t *from) {
+    /* Chunk 2s + lane / 32 of a lane's row: the place of chunk lane / 32 with two bits turned. */
+    const uint32_t ra = place(wm + lane % 32, lane / 32), rb = BM * 128 + place(wn + lane % 32, lane / 32);
+    auto read = [&](uint32_t from, int s) {
+        const uint8_t *at_a = lds + ((ra + from) ^ (s * 32u)), *at_b = lds + ((rb + from) ^ (s * 32u));
 #pragma unroll
-        for (int s = 0; s < 4; s++) {
-            v4i fa[TM], fb[TN];
+        for (int j = 0; j < TN; j++) fb[s & 1][j] = frag(at_b + j * BLOCK);
 #pragma unroll
-            for (int i = 0; i < TM; i++) fa[i] = frag(from, wm + i * 32 + lane % 32, s * 2 + lane / 32);
+        for (int i = 0; i < TM; i++) fa[s & 1][i] = frag(at_a + i * BLOCK);
+    };
+    /* Rows of a result are columns of c, so that a lane holds four neighbours of a row of c. */
+    auto multiply = [&](int s, int from, int to) {
 #pragma unroll
-            for (int j = 0; j < TN; j++) fb[j] = frag(from + BM * 128, wn + j * 32 + lane % 32, s * 2 + lane / 32);
-#pragma unroll
-            for (int i = 0; i < TM; i++)
-#pragma unroll
-                for (int j = 0; j < TN; j++) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa[i], fb[j], acc[i][j], 0, 0, 0);
-        }
+        for (int t = from; t < to; t++)
+            acc[t / TN][t % TN] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[s & 1][t % TN], fa[s & 1][t / TN], acc[t / TN][t % TN], 0, 0, 0);
     };
     fetch(0, lds);
+    wait_loads();
+    wg_sync();
+    if (k > 128u) fetch(128u, lds + STAGE);
+    read(0, 0);
     for (uint32_t k0 = 0, at = 0; k0 < k; k0 += 128u, at ^= STAGE) {
+#pragma unroll
+        for (int s = 0; s < 3; s++) {
+            multiply(s, 0, 1);               /* waits for what it multiplies, so the next reads come after it: they are on their way */
+            __builtin_amdgcn_sched_barrier(0);       /* behind the other products */
+            read(at, s + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(s, 1, TM * TN);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         wait_loads();
-        wg_sync();                           /* this stage is there, and nobody reads the one before it any more */
-        if (k - k0 > 128u) fetch(k0 + 128u, lds + (at ^ STAGE));
-        step(lds + at);
+        wg_sync();                           /* the next stage is there, and this one is in registers everywhere */
+        multiply(3, 0, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        if (k0 + 256u < k) fetch(k0 + 256u, lds + at);
+        read(at ^ STAGE, 0);                 /* behind the last stage: old contents, not used */
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(3, 1, TM * TN);
     }
+    wg_sync();
+    /* Out through LDS, 32 rows of a wavefront's part at a time, so that lines are written whole. */
+    constexpr int COLS = TN * 32, PITCH = COLS * (int)sizeof(T) + 16, LANES = COLS * (int)sizeof(T) / 16, PER = 16 / (int)sizeof(T);
+    static_assert(32 * PITCH * W <= 2 * STAGE, "room for every wavefront");
+    uint8_t *mine = lds + wave * (32 * PITCH);
 #pragma unroll
-    for (int i = 0; i < TM; i++)
+    for (int i = 0; i < TM; i++) {
+        const uint32_t row = wm + i * 32 + lane % 32;
+        const float as = out.as[m0 + min(row, rows_a - 1)];
 #pragma unroll
-        for (int r = 0; r < 16; r++) {
-            const uint32_t row = wm + i * 32 + acc_row(r, lane);
-            if (row < rows_a) {
-                const float as = out.as[m0 + row];
-                T *c = out.c + (m0 + row) * out.ldc;
+        for (int j = 0; j < TN; j++)
 #pragma unroll
-                for (int j = 0; j < TN; j++) {
-                    const uint32_t col = wn + j * 32 + lane % 32;
-                    if (col < rows_b) c[n0 + col] = out.value(acc[i][j][r], as, n0 + col);
+            for (int q = 0; q < 4; q++) {
+                const uint32_t col = j * 32 + q * 8 + lane / 32 * 4;
+                T v[4];
+#pragma unroll
+                for (int e = 0; e < 4; e++) v[e] = out.value(acc[i][j][q * 4 + e], as, min(n0 + wn + col + e, n - 1));
+                __builtin_memcpy(__builtin_assume_aligned(mine + lane % 32 * PITCH + col * sizeof(T), sizeof v), v, sizeof v);
+            }
+#pragma unroll
+        for (int s = 0; s < 32 * LANES / 64; s++) {
+            const uint32_t r = s * (64 / LANES) + lane / LANES, c = lane % LANES * PER, at = wn + c, to = wm + i * 32 + r;
+            T v[PER];
+            __builtin_memcpy(v, __builtin_assume_aligned(mine + r * PITCH + c * sizeof(T), 16), 16);
+            if (to < rows_a) {
+                T *p = out.c + (m0 + to) * out.ldc + n0 + at;
+                if (at + PER <= rows_b) {
+                    Bytes<4> x;
+                    __builtin_memcpy(&x, v, 16);
+                    *reinterpret_cast<Bytes<4> *>(p) = x;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < PER; e++)
+                        if (at + e < rows_b) p[e] = v[e];
                 }
             }
         }
+    }
 }
 
 /* ---------------------------------------------------------------- few rows */

@@ -1,9 +1,10 @@
 /*
  * Tiles in LDS for the matrix instructions, shared by the products and the weight gradient.
  *
- * A tile's row is 128 bytes of the summed dimension (128 codes, or 64 bfloat16) in eight chunks of 16 bytes, chunk c of row r
- * at place c ^ swizzle(r): eight neighbouring rows hold a chunk at eight places, so that the 16-byte reads of a matrix
- * instruction (the same chunk of 32 rows) meet no bank twice.
+ * A tile's row is 128 bytes of the summed dimension (128 codes, or 64 bfloat16) in eight chunks of 16 bytes.  Two neighbouring
+ * rows share 256 bytes, all the banks of LDS once, and their sixteen chunks lie there in an order that is another one for each
+ * of 16 neighbouring pairs, so that the same chunk of 32 rows, which is what a matrix instruction reads, meets every bank equally
+ * often.  Rows 32 apart have the same order: one address per operand and chunk does for all of a wavefront's blocks.
  */
 #ifndef NSML_LAYER8_TILES_HPP
 #define NSML_LAYER8_TILES_HPP
@@ -20,14 +21,14 @@ typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 /* Longest row stride: the rows of a tile lie within 32 bits of its first. */
 constexpr uint64_t MAX_LD = 1u << 22;
 
-__device__ __forceinline__ uint32_t swizzle(uint32_t row) { return (row ^ (row >> 3)) & 7u; }
-__device__ __forceinline__ uint32_t place(uint32_t row, uint32_t chunk) { return row * 128u + ((chunk ^ swizzle(row)) * 16u); }
-
-/* What a lane gives a matrix instruction of 32 x 32: 16 bytes of one row. */
-__device__ __forceinline__ v4i frag(const uint8_t *tile, uint32_t row, uint32_t chunk)
+__device__ __forceinline__ uint32_t place(uint32_t row, uint32_t chunk)
 {
-    return *reinterpret_cast<const v4i *>(tile + place(row, chunk));
+    return row / 2u * 256u + ((((row % 2u) * 8u + chunk) ^ (row / 2u % 16u)) * 16u);
 }
+constexpr uint32_t BLOCK = 32 * 128;                 /* bytes from one block of 32 rows to the next */
+
+/* What a lane gives a matrix instruction of 32 x 32: 16 bytes of one row of a block. */
+__device__ __forceinline__ v4i frag(const uint8_t *at) { return *reinterpret_cast<const v4i *>(at); }
 /* The row of a 32 x 32 result that register r of a lane holds; its column is lane % 32. */
 __device__ __forceinline__ uint32_t acc_row(int r, uint32_t lane) { return (uint32_t)(r % 4 + r / 4 * 8) + lane / 32u * 4u; }
 
@@ -40,8 +41,8 @@ __device__ __forceinline__ void load_tile(const int8_t *from, uint64_t ld, uint3
 {
 #pragma unroll
     for (int i = 0; i < ROWS / 8 / W; i++) {
-        const uint32_t r0 = (i * W + wave) * 8u, row = r0 + lane / 8u;
-        const uint32_t off = min(row, rows - 1) * (uint32_t)ld + ((lane % 8u) ^ swizzle(row)) * 16u;
+        const uint32_t r0 = (i * W + wave) * 8u, pair = r0 / 2u + lane / 16u, at = (lane % 16u) ^ (pair % 16u);
+        const uint32_t off = min(pair * 2u + at / 8u, rows - 1) * (uint32_t)ld + at % 8u * 16u;
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from + off),
                                          (__attribute__((address_space(3))) void *)(to + r0 * 128u), 16, 0, 0);
     }

@@ -13,8 +13,8 @@ namespace {
 template <typename T> constexpr int PARTS = sizeof(T) == 4 ? 3 : 2;
 template <> constexpr int PARTS<bf16> = 1;
 
-/* Words of eight neighbours of dy. */
-template <typename T> constexpr int WORDS = (int)sizeof(T) * 2;
+/* Words of four neighbours of dy. */
+template <typename T> constexpr int WORDS = (int)sizeof(T);
 
 /* Upper halves of two binary32 side by side: bfloat16 where the lower halves are 0, else cut off. */
 __device__ __forceinline__ uint32_t upper2(float lo, float hi) { return __builtin_amdgcn_perm(to_bits(hi), to_bits(lo), 0x07060302u); }
@@ -23,6 +23,29 @@ __device__ __forceinline__ float left_of(float v)
 {
     const float h = from_bits(to_bits(v) & 0xFFFF0000u);
     return h == v ? 0.0f : v - h;
+}
+
+__device__ __forceinline__ void load4(const float *p, int n, float (&v)[4])
+{
+    if (n == 4) {
+        const auto b = *reinterpret_cast<const Bytes<4> *>(p);
+        __builtin_memcpy(v, &b, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) v[i] = i < n ? p[i] : 0.0f;
+    }
+}
+__device__ __forceinline__ void store4(float *p, int n, const float (&v)[4])
+{
+    if (n == 4) {
+        Bytes<4> b;
+        __builtin_memcpy(&b, v, 16);
+        *reinterpret_cast<Bytes<4> *>(p) = b;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            if (i < n) p[i] = v[i];
+    }
 }
 
 template <typename T> struct Wgrad {
@@ -34,146 +57,175 @@ template <typename T> struct Wgrad {
     uint32_t n, k, slices;
 };
 
-/* A tile of BN x BK of dw by WM x WN wavefronts, one slice of the rows, 64 rows to a stage.  Half of the wavefronts bring dy, the
- * other half the codes: the next stage's are on their way to registers while this one's are multiplied. */
-template <typename T, int BN, int BK, int WM, int WN>
+/* A tile of BN x BK of dw by WM x WN wavefronts, one slice of the rows, 64 rows to a stage.  Every thread brings eight rows of four
+ * neighbours of both operands: the next stage's wait in registers while this one is multiplied and go to the other half of
+ * LDS between its matrix instructions, which leave the vector unit three quarters of its time.  Neighbour j of the four goes to row
+ * j * BN / 4 + group of LDS: writes meet no bank twice, and a wavefront whose blocks are the four neighbours of 32 groups holds four
+ * neighbours of dw in a lane.  NARROW: n < 4. */
+template <typename T, int BN, int BK, int WM, int WN, bool NARROW>
 __global__ void __launch_bounds__(WM * WN * 64)
 k_wgrad(Wgrad<T> g)
 {
-    constexpr int P = PARTS<T>, W = WM * WN, TM = BN / WM / 32, TN = BK / WN / 32, HALF = W * 32;
+    constexpr int P = PARTS<T>, W = WM * WN, TM = BN / WM / 32, TN = 4, WD = WORDS<T>;
     constexpr int STAGE = (P * BN + BK) * 128;
-    static_assert(BN == HALF && BK == HALF, "a unit of 8 x 8 per thread");
+    static_assert(BN == W * 32 && BK == BN && BK == WN * 128, "a unit of 8 x 4 of both operands per thread, 128 columns per wavefront");
     __shared__ __align__(16) uint8_t lds[2 * STAGE];
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const Tile tile = tile_of(blockIdx.x, (g.n + BN - 1) / BN, (g.k + BK - 1) / BK);
     const uint32_t n0 = tile.row * BN, k0 = tile.col * BK;
     const uint64_t stages = (g.rows + 63) / 64;
     const uint64_t from = stages * blockIdx.y / g.slices, to = stages * (blockIdx.y + 1) / g.slices;
-    const uint32_t wm = wave / WN * (BN / WM), wn = wave % WN * (BK / WN);
-    const bool brings_dy = wave < W / 2;
-    const uint32_t unit = threadIdx.x % HALF, group = unit % (HALF / 8), chunk = unit / (HALF / 8);
-    uint32_t raw[8][WORDS<T>];
+    const uint32_t wm = wave / WN * (BN / WM), wn = wave % WN * 32u;        /* rows of LDS */
+    const uint32_t group = threadIdx.x % (BN / 4), chunk = threadIdx.x / (BN / 4);
+    /* Columns beyond the matrices: any that are there, as what comes of them is not stored.  The four that a row of dy ends in are read
+     * from the last four, and moved (n >= 4), or one by one. */
+    const uint32_t cd = n0 + group * 4u, cx = k0 + group * 4u;
+    const bool ends = !NARROW && cd < g.n && cd + 4u > g.n;
+    const uint32_t at_d = (cd + 4u <= g.n ? cd : NARROW ? 0u : g.n - 4u) * (uint32_t)sizeof(T);
+    const uint32_t at_x = cx < g.k ? cx : 0u, at_e = at_x / 32u;
+    const uint32_t ld_d = (uint32_t)g.dy.ld * (uint32_t)sizeof(T), ld_x = (uint32_t)g.x.ldq, ld_e = (uint32_t)g.x.lde;
+    uint32_t d[8][WD], q[8], e[8];
 
     auto fetch = [&](uint64_t stage) {
-        const uint64_t row0 = stage * 64 + chunk * 8;
-        if (brings_dy) {
-            const uint32_t c = n0 + group * 8;
-            const int have = c < g.n ? (int)min(g.n - c, 8u) : 0;
+        const uint64_t row0 = stage * 64u;
+        const uint32_t last = (uint32_t)min<uint64_t>(g.rows - row0, 64u) - 1u;
+        const uint8_t *pd = reinterpret_cast<const uint8_t *>(g.dy.p) + row0 * ld_d;
+        const int8_t *px = g.x.q + row0 * ld_x;
+        const uint8_t *pe = g.x.e + row0 * ld_e;
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                if (row0 + i < g.rows && have == 8) {
-                    const auto b = *reinterpret_cast<const Bytes<WORDS<T>> *>(g.dy.at(row0 + i, c));
+        for (int i = 0; i < 8; i++) {
+            const uint32_t row = min(chunk * 8u + i, last);
+            q[i] = *reinterpret_cast<const uint32_t *>(px + (__umul24(row, ld_x) + at_x));
+            e[i] = pe[__umul24(row, ld_e) + at_e];
+            if constexpr (!NARROW) {
+                const auto b = *reinterpret_cast<const Bytes<WD> *>(pd + (__umul24(row, ld_d) + at_d));
 #pragma unroll
-                    for (int w = 0; w < WORDS<T>; w++) raw[i][w] = b.w[w];
-                } else {
-                    T v[8];
+                for (int w = 0; w < WD; w++) d[i][w] = b.w[w];
+            } else {
+                T v[4];
 #pragma unroll
-                    for (int e = 0; e < 8; e++) v[e] = row0 + i < g.rows && e < have ? *g.dy.at(row0 + i, c + e) : (T)0.0f;
-                    __builtin_memcpy(raw[i], v, sizeof v);
-                }
-            }
-        } else {
-            const uint32_t c = k0 + group * 8;
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                uint2 q = make_uint2(0, 0);
-                uint32_t e = 0;
-                if (row0 + i < g.rows && c < g.k) {
-                    q = *reinterpret_cast<const uint2 *>(g.x.q + (row0 + i) * g.x.ldq + c);
-                    e = g.x.e[(row0 + i) * g.x.lde + c / 32u];
-                }
-                raw[i][0] = q.x, raw[i][1] = q.y, raw[i][2] = e;
+                for (uint32_t c = 0; c < 4; c++) v[c] = *reinterpret_cast<const T *>(pd + (__umul24(row, ld_d) + min(c, g.n - 1) * (uint32_t)sizeof(T)));
+                __builtin_memcpy(d[i], v, sizeof v);
             }
         }
     };
-    auto put = [&](uint8_t *stage) {
-        if (brings_dy) {
+    /* What was read is put right where a matrix ends: once per stage, and nothing to do in most. */
+    auto mend = [&](uint64_t stage) {
+        const uint64_t have = g.rows - stage * 64u;
+        if (have < 64u) {
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-                v4i p[P];
-                if constexpr (P == 1) {
+            for (int i = 0; i < 8; i++)
+                if (chunk * 8u + i >= have) {
+                    q[i] = e[i] = 0;
 #pragma unroll
-                    for (int i = 0; i < 4; i++)
-                        p[0][i] = (int)__builtin_amdgcn_perm(raw[2 * i + 1][j / 2], raw[2 * i][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
-                } else {
+                    for (int w = 0; w < WD; w++) d[i][w] = 0;
+                }
+        }
+        if (ends)
+            for (uint32_t s = g.n % 4u; s < 4u; s++)
 #pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        float v[2];
-#pragma unroll
-                        for (int h = 0; h < 2; h++) {
-                            if constexpr (P == 2) v[h] = (float)__builtin_bit_cast(f16, (uint16_t)(raw[2 * i + h][j / 2] >> (j % 2 * 16)));
-                            else v[h] = from_bits(raw[2 * i + h][j]);
-                        }
-#pragma unroll
-                        for (int s = 0; s < P; s++) {
-                            p[s][i] = (int)upper2(v[0], v[1]);
-                            v[0] = left_of(v[0]), v[1] = left_of(v[1]);
-                        }
+                for (int i = 0; i < 8; i++) {
+                    if constexpr (sizeof(T) == 2) {
+                        d[i][0] = __builtin_amdgcn_alignbit(d[i][1], d[i][0], 16);
+                        d[i][1] >>= 16;
+                    } else {
+                        d[i][0] = d[i][1], d[i][1] = d[i][2], d[i][2] = d[i][3];
                     }
                 }
+    };
+    /* Neighbour j of the four, of both operands, as eight rows side by side. */
+    auto put = [&](uint8_t *stage, int j) {
+        v4i p[P];
 #pragma unroll
-                for (int s = 0; s < P; s++) *reinterpret_cast<v4i *>(stage + s * BN * 128 + place(group * 8 + j, chunk)) = p[s];
-            }
-        } else {
-            float s[8];
+        for (int i = 0; i < 4; i++) {
+            if constexpr (P == 1) {
+                p[0][i] = (int)__builtin_amdgcn_perm(d[2 * i + 1][j / 2], d[2 * i][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+            } else {
+                float v[2];
 #pragma unroll
-            for (int i = 0; i < 8; i++) s[i] = ckpt_scale(raw[i][2]);
+                for (int h = 0; h < 2; h++) {
+                    if constexpr (P == 2) v[h] = (float)__builtin_bit_cast(f16, (uint16_t)(d[2 * i + h][j / 2] >> (j % 2 * 16)));
+                    else v[h] = from_bits(d[2 * i + h][j]);
+                }
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-                v4i p;
-#pragma unroll
-                for (int i = 0; i < 4; i++)
-                    p[i] = (int)upper2((float)(int8_t)(raw[2 * i][j / 4] >> (j % 4 * 8)) * s[2 * i],
-                                       (float)(int8_t)(raw[2 * i + 1][j / 4] >> (j % 4 * 8)) * s[2 * i + 1]);
-                *reinterpret_cast<v4i *>(stage + P * BN * 128 + place(group * 8 + j, chunk)) = p;
+                for (int s = 0; s < P; s++) {
+                    p[s][i] = (int)upper2(v[0], v[1]);
+                    v[0] = left_of(v[0]), v[1] = left_of(v[1]);
+                }
             }
         }
+        const uint32_t at = place(j * (BN / 4) + group, chunk);
+#pragma unroll
+        for (int s = 0; s < P; s++) *reinterpret_cast<v4i *>(stage + s * BN * 128 + at) = p[s];
+        v4i x;
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            x[i] = (int)upper2((float)(int8_t)(q[2 * i] >> (j * 8)) * ckpt_scale(e[2 * i]),
+                               (float)(int8_t)(q[2 * i + 1] >> (j * 8)) * ckpt_scale(e[2 * i + 1]));
+        *reinterpret_cast<v4i *>(stage + P * BN * 128 + at) = x;
     };
 
     v16f acc[TM][TN] = {};
-    auto step = [&](const uint8_t *stage) {
+    const uint32_t ra = place(wm + lane % 32, lane / 32), rb = P * BN * 128 + place(wn + lane % 32, lane / 32);
+    auto step = [&](uint32_t stage, int s) {
+        const uint8_t *at_a = lds + ((ra + stage) ^ (s * 32u)), *at_b = lds + ((rb + stage) ^ (s * 32u));
+        v8bf fb[TN];
 #pragma unroll
-        for (int s = 0; s < 4; s++) {
-            v8bf fb[TN];
+        for (int j = 0; j < TN; j++) fb[j] = __builtin_bit_cast(v8bf, frag(at_b + j * (BK / 4 * 128)));
 #pragma unroll
-            for (int j = 0; j < TN; j++) fb[j] = __builtin_bit_cast(v8bf, frag(stage + P * BN * 128, wn + j * 32 + lane % 32, s * 2 + lane / 32));
+        for (int p = P - 1; p >= 0; p--)
 #pragma unroll
-            for (int p = P - 1; p >= 0; p--)
+            for (int i = 0; i < TM; i++) {
+                const v8bf fa = __builtin_bit_cast(v8bf, frag(at_a + p * BN * 128 + i * BLOCK));
 #pragma unroll
-                for (int i = 0; i < TM; i++) {
-                    const v8bf fa = __builtin_bit_cast(v8bf, frag(stage + p * BN * 128, wm + i * 32 + lane % 32, s * 2 + lane / 32));
-#pragma unroll
-                    for (int j = 0; j < TN; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
-                }
-        }
-    };
-    if (from < to) fetch(from);
-    uint32_t at = 0;
-    for (uint64_t stage = from; stage < to; stage++, at ^= STAGE) {
-        put(lds + at);
-        wg_sync();                           /* this stage is there; the other half is read by nobody: all came here after it */
-        if (stage + 1 < to) fetch(stage + 1);
-        step(lds + at);
-    }
-    const uint64_t base = (uint64_t)blockIdx.y * g.n;
-#pragma unroll
-    for (int j = 0; j < TN; j++) {
-        const uint32_t c = k0 + wn + j * 32 + lane % 32;
-        if (c >= g.k) continue;
-        const float s = g.col ? g.col[c] : 1.0f;
-#pragma unroll
-        for (int i = 0; i < TM; i++)
-#pragma unroll
-            for (int r = 0; r < 16; r++) {
-                const uint32_t row = n0 + wm + i * 32 + acc_row(r, lane);
-                if (row >= g.n) continue;
-                if (g.slices > 1) g.part[(base + row) * g.k + c] = acc[i][j][r];
-                else {
-                    const float v = acc[i][j][r] * s;
-                    g.dw[row * g.lddw + c] = g.add ? g.add[row * g.lddw + c] + v : v;
-                }
+                for (int j = 0; j < TN; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
             }
+    };
+    if (from < to) {
+        /* Behind the last stage it is read again, and put where nobody looks: the reads in flight stay in their registers and there
+         * is one copy of the products. */
+        fetch(from);
+        mend(from);
+#pragma unroll
+        for (int j = 0; j < 4; j++) put(lds, j);
+        fetch(min(from + 1, to - 1));
+        uint32_t at = 0;
+        for (uint64_t stage = from; stage < to; stage++, at ^= STAGE) {
+            wg_sync();                       /* this stage is there, and nobody reads the other half any more */
+            step(at, 0);
+            step(at, 1);
+            mend(min(stage + 1, to - 1));
+            put(lds + (at ^ STAGE), 0);
+            put(lds + (at ^ STAGE), 1);
+            step(at, 2);
+            put(lds + (at ^ STAGE), 2);
+            put(lds + (at ^ STAGE), 3);
+            fetch(min(stage + 2, to - 1));
+            step(at, 3);
+        }
     }
+    const uint32_t c = k0 + (wn + lane % 32) * 4u;
+    const int have = c < g.k ? (int)min(g.k - c, 4u) : 0;
+    if (have == 0) return;
+    float s[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+    if (g.col && g.slices == 1)
+#pragma unroll
+        for (int j = 0; j < 4; j++) s[j] = g.col[min(c + j, g.k - 1)];
+    float *to_dw = g.slices > 1 ? g.part + (uint64_t)blockIdx.y * g.n * g.k : g.dw;
+    const float *add = g.slices > 1 ? nullptr : g.add;
+    const uint64_t ld = g.slices > 1 ? g.k : g.lddw;
+#pragma unroll
+    for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            const uint32_t at_row = wm + i * 32 + acc_row(r, lane), row = n0 + at_row % (BN / 4) * 4u + at_row / (BN / 4);
+            if (row >= g.n) continue;
+            float v[4], old[4] = {};
+            if (add) load4(add + row * ld + c, have, old);
+#pragma unroll
+            for (int j = 0; j < 4; j++) v[j] = old[j] + acc[i][j][r] * s[j];
+            store4(to_dw + row * ld + c, have, v);
+        }
 }
 
 /* The slices' sums added up in order. */
@@ -190,22 +242,32 @@ __global__ void __launch_bounds__(256) k_wgrad_sum(const float *part, const floa
     }
 }
 
-constexpr uint32_t SIDE = 128;
-/* Rows are cut into slices where there are fewer tiles than the chip has room for at two a compute unit, but no slice is shorter than two stages. */
-uint32_t slices_of(uint64_t rows, uint32_t n, uint32_t k)
+/* Side of the tiles and number of slices.  Tiles of 256 for bfloat16 where they fill the chip; the parts of the other types take
+ * the room that they would need.  Rows are cut into slices where there are fewer tiles than the chip has room for, but no slice is
+ * shorter than two stages. */
+struct Shape { uint32_t side, slices; uint64_t tiles; };
+Shape shape_of(uint64_t rows, uint32_t n, uint32_t k, bool one_part)
 {
-    const uint64_t tiles = (uint64_t)((n + SIDE - 1) / SIDE) * ((k + SIDE - 1) / SIDE), stages = (rows + 63) / 64;
-    uint64_t s = 512 / tiles;
+    const auto tiles = [&](uint64_t s) { return ((n + s - 1) / s) * ((k + s - 1) / s); };
+    const uint32_t side = one_part && tiles(256) >= 192 ? 256 : 128;
+    const uint64_t stages = (rows + 63) / 64;
+    uint64_t s = (side == 256 ? 256 : 512) / tiles(side);
     if (s > stages / 2) s = stages / 2;
-    return s < 2 ? 1u : (uint32_t)s;
+    return {side, s < 2 ? 1u : (uint32_t)s, tiles(side)};
 }
 
-template <typename T> int launch_wgrad(const Wgrad<T> &g, hipStream_t st)
+template <typename T> int launch_wgrad(const Wgrad<T> &g, const Shape &s, hipStream_t st)
 {
-    const uint64_t tiles = (uint64_t)((g.n + SIDE - 1) / SIDE) * ((g.k + SIDE - 1) / SIDE);
-    k_wgrad<T, 128, 128, 2, 2><<<dim3((uint32_t)tiles, g.slices), 256, 0, st>>>(g);
+    const dim3 grid((uint32_t)s.tiles, s.slices);
+    if constexpr (PARTS<T> == 1) {
+        if (s.side == 256) k_wgrad<T, 256, 256, 4, 2, false><<<grid, 512, 0, st>>>(g);
+    }
+    if (s.side == 128) {
+        if (g.n < 4) k_wgrad<T, 128, 128, 4, 1, true><<<grid, 256, 0, st>>>(g);
+        else k_wgrad<T, 128, 128, 4, 1, false><<<grid, 256, 0, st>>>(g);
+    }
     const int rc = launched();
-    if (rc || g.slices == 1) return rc;
+    if (rc || s.slices == 1) return rc;
     k_wgrad_sum<<<dim3((g.k + 255u) / 256u, g.n < 65535u ? g.n : 65535u), 256, 0, st>>>(g.part, g.col, g.add, g.dw, g.lddw, g.n, g.k, g.slices);
     return launched();
 }
@@ -217,7 +279,8 @@ extern "C" {
 uint64_t nsml_ckpt8_wgrad_work(uint64_t rows, uint32_t n, uint32_t k)
 {
     if (n == 0 || k == 0) return 0;
-    const uint32_t s = slices_of(rows, n, k);
+    /* enough for every type */
+    const uint32_t a = shape_of(rows, n, k, true).slices, b = shape_of(rows, n, k, false).slices, s = a > b ? a : b;
     return s > 1 ? (uint64_t)s * n * k * 4u : 0u;
 }
 
@@ -230,12 +293,12 @@ int nsml_ckpt8_wgrad(const void *dy, int type, uint64_t lddy, const nsml_ckpt8 *
         return NSML_EINVAL;
     const uint64_t need = nsml_ckpt8_wgrad_work(rows, n, k);
     if (need && (!work || !at_multiple(work, 16) || work_bytes < need)) return NSML_EINVAL;
-    if ((uint64_t)((n + SIDE - 1) / SIDE) * ((k + SIDE - 1) / SIDE) >= (1u << 24)) return NSML_ECAP;
+    const Shape s = shape_of(rows, n, k, type == NSML_BF16);
+    if (s.tiles >= (1u << 24) || (rows && (lddy >= MAX_LD || x->ldq >= MAX_LD || x->lde >= MAX_LD))) return NSML_ECAP;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const uint32_t slices = slices_of(rows, n, k);
     const auto go = [&](auto v) {
         using T = decltype(v);
-        return launch_wgrad(Wgrad<T>{mat<T>(dy, lddy), ckpt_of(x), col_scale, add, dw, static_cast<float *>(work), lddw, rows, n, k, slices}, st);
+        return launch_wgrad(Wgrad<T>{mat<T>(dy, lddy), ckpt_of(x), col_scale, add, dw, static_cast<float *>(work), lddw, rows, n, k, s.slices}, s, st);
     };
     if (type == NSML_F32) return go(float{});
     if (type == NSML_BF16) return go(bf16{});
