@@ -24,78 +24,117 @@ template <typename T> struct Out {
 
 /* ---------------------------------------------------------------- tiles */
 
-/* A tile of BM x BN by WM x WN wavefronts; k in stages of 128 bytes, loaded straight into LDS one stage ahead.
- * The matrix instructions of the last quarter of a stage run while the first quarter of the next is read from LDS: the barrier
- * between stages stands before them, when all of the stage is in registers. */
+/* A stage of a tile in LDS: 64 bytes of k of each row, four rows to 256 bytes (all the banks once), whose sixteen chunks of 16 bytes
+ * lie there in an order that is another one for each of four neighbouring fours: the same chunk of 16 rows meets every bank once. */
+constexpr uint32_t DEPTH = 64;
+__device__ __forceinline__ uint32_t spot(uint32_t row, uint32_t chunk) { return row / 4u * 256u + (((row % 4u * 4u + chunk) ^ (row / 4u % 4u)) * 16u); }
+
+/* A tile of BM x BN by WM x WN wavefronts.  Stages go from memory straight into a ring of four places in LDS, three ahead; a wavefront's
+ * requests are spread between its matrix instructions, as one that waits to make a request multiplies nothing.  The matrix instructions of
+ * a stage's second half run while the next stage's first half is read from LDS: the barrier between stages stands before them,
+ * when all of the stage is in registers. */
 template <typename T, int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(WM * WN * 64)
 k_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t m, uint32_t n, uint32_t k, Out<T> out)
 {
-    constexpr int W = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
-    constexpr int STAGE = (BM + BN) * 128;
-    __shared__ __align__(16) uint8_t lds[2 * STAGE];
+    constexpr int W = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, LA = BM / 16 / W, LB = BN / 16 / W, L = LA + LB;
+    constexpr uint32_t STAGE = (BM + BN) * DEPTH, RING = 4;
+    static_assert(LA >= 1 && LB >= 1 && (TM * TN >= L || TM * TN == 1), "a request between two matrix instructions");
+    __shared__ __align__(16) uint8_t lds[RING * STAGE];
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const Tile tile = tile_of(blockIdx.x, (uint32_t)((m + BM - 1) / BM), (n + BN - 1) / BN);
     const uint64_t m0 = (uint64_t)tile.row * BM;
     const uint32_t n0 = tile.col * BN;
     const uint32_t rows_a = (uint32_t)min<uint64_t>(m - m0, BM), rows_b = min(n - n0, (uint32_t)BN);
     const uint32_t wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+    const int8_t *pa = a + m0 * lda, *pb = b + (uint64_t)n0 * ldb;
     v16i acc[TM][TN] = {};
     v4i fa[2][TM], fb[2][TN];
-    const int8_t *pa = a + m0 * lda, *pb = b + (uint64_t)n0 * ldb;
-    auto fetch = [&](uint32_t k0, uint8_t *to) {
-        if (k - k0 >= 128u) {
-            load_tile<BM, W>(pa + k0, lda, rows_a, to, wave, lane);
-            load_tile<BN, W>(pb + k0, ldb, rows_b, to + BM * 128, wave, lane);
-        } else {
-            load_tail<BM, W>(pa + k0, lda, rows_a, k - k0, to, threadIdx.x);
-            load_tail<BN, W>(pb + k0, ldb, rows_b, k - k0, to + BM * 128, threadIdx.x);
-        }
+
+    /* A request brings 16 rows; rows beyond the matrix are its last one again.  Chunks beyond a row's end (in the last stage) are the
+     * stage's first again: what they hold is multiplied by zeros. */
+    uint32_t off[L], chunk[L];
+#pragma unroll
+    for (int l = 0; l < L; l++) {
+        const uint32_t four = ((l < LA ? l : l - LA) * W + wave) * 4u + lane / 16u, at = (lane % 16u) ^ (four % 4u);
+        const uint32_t row = min(four * 4u + at / 4u, (l < LA ? rows_a : rows_b) - 1u);
+        chunk[l] = at % 4u * 16u;
+        off[l] = row * (uint32_t)(l < LA ? lda : ldb);
+    }
+    const uint32_t stages = (k + DEPTH - 1) / DEPTH;
+    auto request = [&](uint32_t stage, int l) {
+        const uint32_t k0 = min(stage, stages - 1u) * DEPTH;
+        const uint32_t at = off[l] + (k0 + chunk[l] < k ? chunk[l] : 0u);
+        uint8_t *to = lds + stage % RING * STAGE + (l < LA ? 0u : BM * DEPTH) + ((l < LA ? l : l - LA) * W + wave) * 1024u;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)((l < LA ? pa : pb) + k0 + at),
+                                         (__attribute__((address_space(3))) void *)to, 16, 0, 0);
     };
-    /* Chunk 2s + lane / 32 of a lane's row: the place of chunk lane / 32 with two bits turned. */
-    const uint32_t ra = place(wm + lane % 32, lane / 32), rb = BM * 128 + place(wn + lane % 32, lane / 32);
-    auto read = [&](uint32_t from, int s) {
+    /* Chunk 2s + lane / 32 of a lane's row: the place of chunk lane / 32 with a bit turned. */
+    const uint32_t ra = spot(wm + lane % 32, lane / 32), rb = BM * DEPTH + spot(wn + lane % 32, lane / 32);
+    auto read = [&](uint32_t stage, int s) {
+        const uint32_t from = stage % RING * STAGE;
         const uint8_t *at_a = lds + ((ra + from) ^ (s * 32u)), *at_b = lds + ((rb + from) ^ (s * 32u));
 #pragma unroll
-        for (int j = 0; j < TN; j++) fb[s & 1][j] = frag(at_b + j * BLOCK);
+        for (int j = 0; j < TN; j++) fb[s][j] = frag(at_b + j * (32 * DEPTH));
 #pragma unroll
-        for (int i = 0; i < TM; i++) fa[s & 1][i] = frag(at_a + i * BLOCK);
+        for (int i = 0; i < TM; i++) fa[s][i] = frag(at_a + i * (32 * DEPTH));
     };
     /* Rows of a result are columns of c, so that a lane holds four neighbours of a row of c. */
-    auto multiply = [&](int s, int from, int to) {
-#pragma unroll
-        for (int t = from; t < to; t++)
-            acc[t / TN][t % TN] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[s & 1][t % TN], fa[s & 1][t / TN], acc[t / TN][t % TN], 0, 0, 0);
+    auto multiply = [&](int s, int t) {
+        acc[t / TN][t % TN] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[s][t % TN], fa[s][t / TN], acc[t / TN][t % TN], 0, 0, 0);
     };
-    fetch(0, lds);
-    wait_loads();
-    wg_sync();
-    if (k > 128u) fetch(128u, lds + STAGE);
-    read(0, 0);
-    for (uint32_t k0 = 0, at = 0; k0 < k; k0 += 128u, at ^= STAGE) {
+    auto cut = [&](int s) {                  /* the last stage: zeros from k on */
 #pragma unroll
-        for (int s = 0; s < 3; s++) {
-            multiply(s, 0, 1);               /* waits for what it multiplies, so the next reads come after it: they are on their way */
-            __builtin_amdgcn_sched_barrier(0);       /* behind the other products */
-            read(at, s + 1);
-            __builtin_amdgcn_sched_barrier(0);
-            multiply(s, 1, TM * TN);
+        for (int i = 0; i < TM; i++) fa[s][i] = first_bytes(fa[s][i], (int)(k - (stages - 1u) * DEPTH) - (int)(s * 32u + lane / 32u * 16u));
+    };
+
+#pragma unroll
+    for (uint32_t r = 0; r < RING - 1; r++)
+#pragma unroll
+        for (int l = 0; l < L; l++) request(r, l);
+    loads_sync<2 * L>();
+    read(0, 0);
+    for (uint32_t stage = 0; stage < stages; stage++) {
+        const bool ends = stage + 1 == stages && k % DEPTH;
+        wait_lds();
+        if (ends) cut(0);
+        multiply(0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        read(stage, 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 1; t < TM * TN; t++) {
+            multiply(0, t);
+            if (t - 1 < L) request(stage + RING - 1, t - 1);
             __builtin_amdgcn_sched_barrier(0);
         }
-        wait_loads();
-        wg_sync();                           /* the next stage is there, and this one is in registers everywhere */
-        multiply(3, 0, 1);
+        if (TM * TN - 1 < L)
+#pragma unroll
+            for (int l = TM * TN - 1; l < L; l++) request(stage + RING - 1, l);
+        loads_sync<2 * L>();                 /* the next stage is there (two more may be on their way), this one is in registers everywhere */
+        if (ends) cut(1);
+        multiply(1, 0);
         __builtin_amdgcn_sched_barrier(0);
-        if (k0 + 256u < k) fetch(k0 + 256u, lds + at);
-        read(at ^ STAGE, 0);                 /* behind the last stage: old contents, not used */
+        read(stage + 1, 0);                  /* behind the last stage: its contents again, not used */
         __builtin_amdgcn_sched_barrier(0);
-        multiply(3, 1, TM * TN);
+#pragma unroll
+        for (int t = 1; t < TM * TN; t++) multiply(1, t);
+        __builtin_amdgcn_sched_barrier(0);
     }
-    wg_sync();
+    loads_sync<0>();
     /* Out through LDS, 32 rows of a wavefront's part at a time, so that lines are written whole. */
     constexpr int COLS = TN * 32, PITCH = COLS * (int)sizeof(T) + 16, LANES = COLS * (int)sizeof(T) / 16, PER = 16 / (int)sizeof(T);
-    static_assert(32 * PITCH * W <= 2 * STAGE, "room for every wavefront");
+    static_assert(32 * PITCH * W <= RING * STAGE, "room for every wavefront");
     uint8_t *mine = lds + wave * (32 * PITCH);
+    float bs[TN][16], bias[TN][16];
+#pragma unroll
+    for (int j = 0; j < TN; j++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+            const uint32_t col = min(n0 + wn + j * 32 + acc_row(e, lane), n - 1);
+            bs[j][e] = out.bs ? out.bs[col] : 1.0f;
+            bias[j][e] = out.bias ? out.bias[col] : 0.0f;
+        }
 #pragma unroll
     for (int i = 0; i < TM; i++) {
         const uint32_t row = wm + i * 32 + lane % 32;
@@ -107,7 +146,7 @@ k_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t
                 const uint32_t col = j * 32 + q * 8 + lane / 32 * 4;
                 T v[4];
 #pragma unroll
-                for (int e = 0; e < 4; e++) v[e] = out.value(acc[i][j][q * 4 + e], as, min(n0 + wn + col + e, n - 1));
+                for (int e = 0; e < 4; e++) v[e] = (T)((float)acc[i][j][q * 4 + e] * as * bs[j][q * 4 + e] + bias[j][q * 4 + e]);
                 __builtin_memcpy(__builtin_assume_aligned(mine + lane % 32 * PITCH + col * sizeof(T), sizeof v), v, sizeof v);
             }
 #pragma unroll

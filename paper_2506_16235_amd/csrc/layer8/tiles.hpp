@@ -32,20 +32,17 @@ __device__ __forceinline__ v4i frag(const uint8_t *at) { return *reinterpret_cas
 /* The row of a 32 x 32 result that register r of a lane holds; its column is lane % 32. */
 __device__ __forceinline__ uint32_t acc_row(int r, uint32_t lane) { return (uint32_t)(r % 4 + r / 4 * 8) + lane / 32u * 4u; }
 
-__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }       /* vmcnt(0) */
-
-/* ROWS x 128 bytes from memory straight into LDS by W wavefronts: eight rows per instruction, lanes permuted within their row.
- * Rows beyond `rows` are given the last one's contents. */
-template <int ROWS, int W>
-__device__ __forceinline__ void load_tile(const int8_t *from, uint64_t ld, uint32_t rows, uint8_t *to, uint32_t wave, uint32_t lane)
+/* Until this wavefront's reads of LDS are done. */
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F); }
+/* Until at most N of this wavefront's loads are on their way, and its accesses to LDS are done; then until all wavefronts are here.
+ * (__syncthreads would wait for every load that goes straight to LDS.) */
+template <int N> __device__ __forceinline__ void loads_sync()
 {
-#pragma unroll
-    for (int i = 0; i < ROWS / 8 / W; i++) {
-        const uint32_t r0 = (i * W + wave) * 8u, pair = r0 / 2u + lane / 16u, at = (lane % 16u) ^ (pair % 16u);
-        const uint32_t off = min(pair * 2u + at / 8u, rows - 1) * (uint32_t)ld + at % 8u * 16u;
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from + off),
-                                         (__attribute__((address_space(3))) void *)(to + r0 * 128u), 16, 0, 0);
-    }
+    static_assert(N < 64, "six bits");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4 << 14));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
 }
 
 /* The first n bytes of a chunk, zeros after them. */
@@ -57,20 +54,6 @@ __device__ __forceinline__ v4i first_bytes(v4i v, int n)
         v[i] = have >= 4 ? v[i] : have <= 0 ? 0 : (int)((uint32_t)v[i] & ((1u << (8 * have)) - 1u));
     }
     return v;
-}
-
-/* The last stage of rows that end within it, `bytes` (< 128) of each: through registers, with zeros from there on.  Nothing is
- * read beyond the chunk of 16 bytes that a row ends in. */
-template <int ROWS, int W>
-__device__ __forceinline__ void load_tail(const int8_t *from, uint64_t ld, uint32_t rows, uint32_t bytes, uint8_t *to, uint32_t thread)
-{
-#pragma unroll
-    for (uint32_t i = thread; i < ROWS * 8u; i += W * 64u) {
-        const uint32_t row = i / 8u, chunk = i % 8u;
-        v4i v = {};
-        if (chunk * 16u < bytes) v = first_bytes(*reinterpret_cast<const v4i *>(from + min(row, rows - 1) * (uint32_t)ld + chunk * 16u), (int)(bytes - chunk * 16u));
-        *reinterpret_cast<v4i *>(to + place(row, chunk)) = v;
-    }
 }
 
 /* Which tile a workgroup takes.  Workgroups go round the eight dies; each die gets a run of neighbouring tiles, in bands of
