@@ -29,22 +29,18 @@ template <typename T> struct Out {
 constexpr uint32_t DEPTH = 64;
 __device__ __forceinline__ uint32_t spot(uint32_t row, uint32_t chunk) { return row / 4u * 256u + (((row % 4u * 4u + chunk) ^ (row / 4u % 4u)) * 16u); }
 
-/* A tile of BM x BN by WM x WN wavefronts.  Stages go from memory straight into a ring of four places in LDS, three ahead; a wavefront's
+/* A tile of BM x BN by WM x WN wavefronts.  Stages go from memory straight into a ring of places in LDS, all but one ahead; a wavefront's
  * requests are spread between its matrix instructions, as one that waits to make a request multiplies nothing.  The matrix instructions of
  * a stage's second half run while the next stage's first half is read from LDS: the barrier between stages stands before them,
  * when all of the stage is in registers. */
-template <typename T, int BM, int BN, int WM, int WN>
-__global__ void __launch_bounds__(WM * WN * 64)
-k_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t m, uint32_t n, uint32_t k, Out<T> out)
+template <typename T, int BM, int BN, int WM, int WN, int RING>
+__device__ __forceinline__ void product_tile(uint8_t *lds, uint64_t m0, uint32_t n0, const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb,
+                                             uint64_t m, uint32_t n, uint32_t k, const Out<T> &out)
 {
     constexpr int W = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, LA = BM / 16 / W, LB = BN / 16 / W, L = LA + LB;
-    constexpr uint32_t STAGE = (BM + BN) * DEPTH, RING = 4;
+    constexpr uint32_t STAGE = (BM + BN) * DEPTH;
     static_assert(LA >= 1 && LB >= 1 && (TM * TN >= L || TM * TN == 1), "a request between two matrix instructions");
-    __shared__ __align__(16) uint8_t lds[RING * STAGE];
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
-    const Tile tile = tile_of(blockIdx.x, (uint32_t)((m + BM - 1) / BM), (n + BN - 1) / BN);
-    const uint64_t m0 = (uint64_t)tile.row * BM;
-    const uint32_t n0 = tile.col * BN;
     const uint32_t rows_a = (uint32_t)min<uint64_t>(m - m0, BM), rows_b = min(n - n0, (uint32_t)BN);
     const uint32_t wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
     const int8_t *pa = a + m0 * lda, *pb = b + (uint64_t)n0 * ldb;
@@ -62,17 +58,16 @@ k_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t
         off[l] = row * (uint32_t)(l < LA ? lda : ldb);
     }
     const uint32_t stages = (k + DEPTH - 1) / DEPTH;
-    auto request = [&](uint32_t stage, int l) {
+    auto request = [&](uint32_t stage, uint32_t ring, int l) {
         const uint32_t k0 = min(stage, stages - 1u) * DEPTH;
         const uint32_t at = off[l] + (k0 + chunk[l] < k ? chunk[l] : 0u);
-        uint8_t *to = lds + stage % RING * STAGE + (l < LA ? 0u : BM * DEPTH) + ((l < LA ? l : l - LA) * W + wave) * 1024u;
+        uint8_t *to = lds + ring + (l < LA ? 0u : BM * DEPTH) + ((l < LA ? l : l - LA) * W + wave) * 1024u;
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)((l < LA ? pa : pb) + k0 + at),
                                          (__attribute__((address_space(3))) void *)to, 16, 0, 0);
     };
     /* Chunk 2s + lane / 32 of a lane's row: the place of chunk lane / 32 with a bit turned. */
     const uint32_t ra = spot(wm + lane % 32, lane / 32), rb = BM * DEPTH + spot(wn + lane % 32, lane / 32);
-    auto read = [&](uint32_t stage, int s) {
-        const uint32_t from = stage % RING * STAGE;
+    auto read = [&](uint32_t from, int s) {
         const uint8_t *at_a = lds + ((ra + from) ^ (s * 32u)), *at_b = lds + ((rb + from) ^ (s * 32u));
 #pragma unroll
         for (int j = 0; j < TN; j++) fb[s][j] = frag(at_b + j * (32 * DEPTH));
@@ -91,35 +86,40 @@ k_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t
 #pragma unroll
     for (uint32_t r = 0; r < RING - 1; r++)
 #pragma unroll
-        for (int l = 0; l < L; l++) request(r, l);
-    loads_sync<2 * L>();
+        for (int l = 0; l < L; l++) request(r, r * STAGE, l);
+    constexpr int LATER = (RING - 2) * L;    /* requests that may be on their way when the next stage has to be there */
+    loads_sync<LATER>();
     read(0, 0);
+    uint32_t here = 0, there = (RING - 1) * STAGE;       /* the stage's place, and the one before it, which is free */
     for (uint32_t stage = 0; stage < stages; stage++) {
+        const uint32_t next = here + STAGE == RING * STAGE ? 0u : here + STAGE;
         const bool ends = stage + 1 == stages && k % DEPTH;
         wait_lds();
         if (ends) cut(0);
         multiply(0, 0);
         __builtin_amdgcn_sched_barrier(0);
-        read(stage, 1);
+        read(here, 1);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int t = 1; t < TM * TN; t++) {
             multiply(0, t);
-            if (t - 1 < L) request(stage + RING - 1, t - 1);
+            if (t - 1 < L) request(stage + RING - 1, there, t - 1);
             __builtin_amdgcn_sched_barrier(0);
         }
         if (TM * TN - 1 < L)
 #pragma unroll
-            for (int l = TM * TN - 1; l < L; l++) request(stage + RING - 1, l);
-        loads_sync<2 * L>();                 /* the next stage is there (two more may be on their way), this one is in registers everywhere */
+            for (int l = TM * TN - 1; l < L; l++) request(stage + RING - 1, there, l);
+        loads_sync<LATER>();                 /* the next stage is there, and this one is in registers everywhere */
         if (ends) cut(1);
         multiply(1, 0);
         __builtin_amdgcn_sched_barrier(0);
-        read(stage + 1, 0);                  /* behind the last stage: its contents again, not used */
+        read(next, 0);                       /* behind the last stage: its contents again, not used */
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int t = 1; t < TM * TN; t++) multiply(1, t);
         __builtin_amdgcn_sched_barrier(0);
+        there = here;
+        here = next;
     }
     loads_sync<0>();
     /* Out through LDS, 32 rows of a wavefront's part at a time, so that lines are written whole. */
@@ -167,6 +167,33 @@ k_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t
                 }
             }
         }
+    }
+}
+
+template <typename T, int SIDE, int RING>
+__global__ void __launch_bounds__(256)
+k_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t m, uint32_t n, uint32_t k, Out<T> out)
+{
+    __shared__ __align__(16) uint8_t lds[RING * 2 * SIDE * DEPTH];
+    const Tile tile = tile_of(blockIdx.x, (uint32_t)((m + SIDE - 1) / SIDE), (n + SIDE - 1) / SIDE);
+    product_tile<T, SIDE, SIDE, 2, 2, RING>(lds, (uint64_t)tile.row * SIDE, tile.col * SIDE, a, lda, b, ldb, m, n, k, out);
+}
+
+/* Tiles of 256 x 256, one workgroup a compute unit.  Those from `whole` on, which would leave half of the chip or more without work
+ * in the last round, are two workgroups each, 128 x 256. */
+template <typename T>
+__global__ void __launch_bounds__(512, 2)
+k_product_large(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t m, uint32_t n, uint32_t k, Out<T> out, uint32_t whole)
+{
+    __shared__ __align__(16) uint8_t lds[4 * 512 * DEPTH];
+    const uint32_t id = blockIdx.x, rows = (uint32_t)((m + 255) / 256), cols = (n + 255) / 256;
+    if (id < whole) {
+        const Tile tile = tile_of(id, rows, cols);
+        product_tile<T, 256, 256, 2, 4, 4>(lds, (uint64_t)tile.row * 256, tile.col * 256u, a, lda, b, ldb, m, n, k, out);
+    } else {
+        const Tile tile = tile_of(whole + (id - whole) / 2u, rows, cols);
+        const uint64_t m0 = (uint64_t)tile.row * 256 + (id - whole) % 2u * 128u;
+        if (m0 < m) product_tile<T, 128, 256, 2, 4, 4>(lds, m0, tile.col * 256u, a, lda, b, ldb, m, n, k, out);
     }
 }
 
@@ -241,12 +268,13 @@ int launch_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb,
     }
     const auto tiles = [&](uint64_t s) { return ((m + s - 1) / s) * ((n + s - 1) / s); };
     if (tiles(256) >= (1u << 24)) return NSML_ECAP;
-    if (tiles(256) >= 256)
-        k_product<T, 256, 256, 2, 4><<<(uint32_t)tiles(256), 512, 0, st>>>(a, lda, b, ldb, m, n, k, out);
+    const uint32_t large = (uint32_t)tiles(256), rest = large % 256u, whole = rest <= 128u ? large - rest : large;
+    if (large >= 96)
+        k_product_large<T><<<whole + (large - whole) * 2u, 512, 0, st>>>(a, lda, b, ldb, m, n, k, out, whole);
     else if (tiles(128) >= 256)
-        k_product<T, 128, 128, 2, 2><<<(uint32_t)tiles(128), 256, 0, st>>>(a, lda, b, ldb, m, n, k, out);
+        k_product<T, 128, 4><<<(uint32_t)tiles(128), 256, 0, st>>>(a, lda, b, ldb, m, n, k, out);
     else
-        k_product<T, 64, 64, 2, 2><<<(uint32_t)tiles(64), 256, 0, st>>>(a, lda, b, ldb, m, n, k, out);
+        k_product<T, 64, 4><<<(uint32_t)tiles(64), 256, 0, st>>>(a, lda, b, ldb, m, n, k, out);
     return launched();
 }
 
