@@ -8,6 +8,8 @@
  */
 #include "tiles.hpp"
 
+#include <type_traits>
+
 namespace {
 
 template <typename T> constexpr int PARTS = sizeof(T) == 4 ? 3 : 2;
@@ -48,6 +50,12 @@ __device__ __forceinline__ void store4(float *p, int n, const float (&v)[4])
     }
 }
 
+typedef const __attribute__((address_space(1))) uint8_t *Global;
+/* Words at an address of any alignment. */
+typedef uint32_t Loose2 __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t Loose4 __attribute__((ext_vector_type(4), aligned(1)));
+template <int N> using Loose = std::conditional_t<N == 2, Loose2, Loose4>;
+
 template <typename T> struct Wgrad {
     Mat<const T> dy;
     Ckpt x;
@@ -86,30 +94,41 @@ k_wgrad(Wgrad<T> g)
     const uint32_t ld_d = (uint32_t)g.dy.ld * (uint32_t)sizeof(T), ld_x = (uint32_t)g.x.ldq, ld_e = (uint32_t)g.x.lde;
     uint32_t d[8][WD], q[8], e[8];
 
-    auto fetch = [&](uint64_t stage) {
+    /* Where a thread's first row lies; the others are whole rows away, which is the same for all threads. */
+    const uint32_t to_d = __umul24(chunk * 8u, ld_d) + at_d, to_x = __umul24(chunk * 8u, ld_x) + at_x, to_e = __umul24(chunk * 8u, ld_e) + at_e;
+    auto fetch = [&](uint64_t stage, auto edge) {
         const uint64_t row0 = stage * 64u;
-        const uint32_t last = (uint32_t)min<uint64_t>(g.rows - row0, 64u) - 1u;
         const uint8_t *pd = reinterpret_cast<const uint8_t *>(g.dy.p) + row0 * ld_d;
-        const int8_t *px = g.x.q + row0 * ld_x;
+        const uint8_t *px = reinterpret_cast<const uint8_t *>(g.x.q) + row0 * ld_x;
         const uint8_t *pe = g.x.e + row0 * ld_e;
+        const uint32_t last = (uint32_t)min<uint64_t>(g.rows - row0, 64u) - 1u;
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            const uint32_t row = min(chunk * 8u + i, last);
-            q[i] = *reinterpret_cast<const uint32_t *>(px + (__umul24(row, ld_x) + at_x));
-            e[i] = pe[__umul24(row, ld_e) + at_e];
+            Global rd = (Global)(pd + i * ld_d), rx = (Global)(px + i * ld_x), re = (Global)(pe + i * ld_e);
+            if constexpr (!edge.value) {
+                uint32_t od = to_d, ox = to_x, oe = to_e;
+                asm("" : "+s"(rd), "+s"(rx), "+s"(re));      /* a row's address is the same for all threads, and what a thread adds fits */
+                asm("" : "+v"(od), "+v"(ox), "+v"(oe));      /* the load itself: no addition of 64 bits per load */
+                rd += od, rx += ox, re += oe;
+            } else {                         /* rows beyond the matrix: its last one */
+                const uint32_t row = min(chunk * 8u + i, last);
+                rd = (Global)pd + (__umul24(row, ld_d) + at_d), rx = (Global)px + (__umul24(row, ld_x) + at_x), re = (Global)pe + (__umul24(row, ld_e) + at_e);
+            }
+            q[i] = *(const __attribute__((address_space(1))) uint32_t *)rx;
+            e[i] = *re;
             if constexpr (!NARROW) {
-                const auto b = *reinterpret_cast<const Bytes<WD> *>(pd + (__umul24(row, ld_d) + at_d));
+                const Loose<WD> b = *(const __attribute__((address_space(1))) Loose<WD> *)rd;
 #pragma unroll
-                for (int w = 0; w < WD; w++) d[i][w] = b.w[w];
+                for (int w = 0; w < WD; w++) d[i][w] = b[w];
             } else {
                 T v[4];
 #pragma unroll
-                for (uint32_t c = 0; c < 4; c++) v[c] = *reinterpret_cast<const T *>(pd + (__umul24(row, ld_d) + min(c, g.n - 1) * (uint32_t)sizeof(T)));
+                for (uint32_t c = 0; c < 4; c++) v[c] = *(const __attribute__((address_space(1))) T *)(rd + min(c, g.n - 1) * (uint32_t)sizeof(T));
                 __builtin_memcpy(d[i], v, sizeof v);
             }
         }
     };
-    /* What was read is put right where a matrix ends: once per stage, and nothing to do in most. */
+    /* What was read where a matrix ends: rows beyond it become zeros, the four that a row of dy ends in were read with those before. */
     auto mend = [&](uint64_t stage) {
         const uint64_t have = g.rows - stage * 64u;
         if (have < 64u) {
@@ -167,42 +186,73 @@ k_wgrad(Wgrad<T> g)
 
     v16f acc[TM][TN] = {};
     const uint32_t ra = place(wm + lane % 32, lane / 32), rb = P * BN * 128 + place(wn + lane % 32, lane / 32);
-    auto step = [&](uint32_t stage, int s) {
+    v8bf fa[2][P][TM], fb[2][TN];
+    auto read = [&](uint32_t stage, int s) {
         const uint8_t *at_a = lds + ((ra + stage) ^ (s * 32u)), *at_b = lds + ((rb + stage) ^ (s * 32u));
-        v8bf fb[TN];
 #pragma unroll
-        for (int j = 0; j < TN; j++) fb[j] = __builtin_bit_cast(v8bf, frag(at_b + j * (BK / 4 * 128)));
+        for (int j = 0; j < TN; j++) fb[s & 1][j] = __builtin_bit_cast(v8bf, frag(at_b + j * (BK / 4 * 128)));
 #pragma unroll
-        for (int p = P - 1; p >= 0; p--)
+        for (int p = 0; p < P; p++)
 #pragma unroll
-            for (int i = 0; i < TM; i++) {
-                const v8bf fa = __builtin_bit_cast(v8bf, frag(at_a + p * BN * 128 + i * BLOCK));
-#pragma unroll
-                for (int j = 0; j < TN; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
-            }
+            for (int i = 0; i < TM; i++) fa[s & 1][p][i] = __builtin_bit_cast(v8bf, frag(at_a + p * BN * 128 + i * BLOCK));
     };
-    if (from < to) {
-        /* Behind the last stage it is read again, and put where nobody looks: the reads in flight stay in their registers and there
-         * is one copy of the products. */
-        fetch(from);
-        mend(from);
+    /* The smallest parts first. */
+    auto multiply = [&](int s, int from, int to) {
+#pragma unroll
+        for (int t = from; t < to; t++) {
+            const int p = P - 1 - t / (TM * TN), i = t / TN % TM, j = t % TN;
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[s & 1][p][i], fb[s & 1][j], acc[i][j], 0, 0, 0);
+        }
+    };
+    constexpr int ALL = P * TM * TN;
+    /* One quarter of a stage: its first product waits for what it multiplies, the next quarter is read behind the others, with
+     * `work` for the vector unit between them. */
+    auto quarter = [&](uint32_t next, int s, auto work) {
+        wait_lds();
+        multiply(s, 0, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        read(next, (s + 1) % 4);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(s, 1, ALL);
+        work();
+    };
+    /* What the vector unit does in a quarter goes between its products, some instructions behind each. */
+    auto between = [&]() {
+#pragma unroll
+        for (int t = 1; t < ALL; t++) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    /* edge: the tile or the slice holds an end of the matrices. */
+    auto all = [&](auto edge) {
+        fetch(from, edge);
+        if constexpr (edge.value) mend(from);
 #pragma unroll
         for (int j = 0; j < 4; j++) put(lds, j);
-        fetch(min(from + 1, to - 1));
+        /* Behind the last stage it is read again, and put where nobody looks: one copy of everything. */
+        fetch(min(from + 1, to - 1), edge);
+        wg_sync();
+        read(0, 0);
         uint32_t at = 0;
         for (uint64_t stage = from; stage < to; stage++, at ^= STAGE) {
-            wg_sync();                       /* this stage is there, and nobody reads the other half any more */
-            step(at, 0);
-            step(at, 1);
-            mend(min(stage + 1, to - 1));
-            put(lds + (at ^ STAGE), 0);
-            put(lds + (at ^ STAGE), 1);
-            step(at, 2);
-            put(lds + (at ^ STAGE), 2);
-            put(lds + (at ^ STAGE), 3);
-            fetch(min(stage + 2, to - 1));
-            step(at, 3);
+            quarter(at, 0, [] {});
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (edge.value) mend(min(stage + 1, to - 1));
+            quarter(at, 1, [&] { put(lds + (at ^ STAGE), 0); put(lds + (at ^ STAGE), 1); });
+            between();
+            quarter(at, 2, [&] { put(lds + (at ^ STAGE), 2); put(lds + (at ^ STAGE), 3); });
+            between();
+            wg_sync();                       /* the next stage is there, and this one is in registers everywhere */
+            fetch(min(stage + 2, to - 1), edge);         /* (between the products: the same within 2 %) */
+            __builtin_amdgcn_sched_barrier(0);
+            quarter(at ^ STAGE, 3, [] {});
         }
+    };
+    if (from < to) {
+        if (NARROW || n0 + BN > g.n || to * 64u > g.rows) all(std::true_type{});
+        else all(std::false_type{});
     }
     const uint32_t c = k0 + (wn + lane % 32) * 4u;
     const int have = c < g.k ? (int)min(g.k - c, 4u) : 0;
