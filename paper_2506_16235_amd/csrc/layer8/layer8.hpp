@@ -61,6 +61,33 @@ template <typename T> __device__ __forceinline__ void store8(T *p, int n, const 
     }
 }
 
+/* Four, the ones from n on left alone. */
+__device__ __forceinline__ void load4(const float *p, int n, float (&v)[4])
+{
+    if (n == 4) {
+        const auto b = *reinterpret_cast<const Bytes<4> *>(p);
+        __builtin_memcpy(v, &b, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) v[i] = i < n ? p[i] : 0.0f;
+    }
+}
+template <typename T> __device__ __forceinline__ void store4(T *p, int n, const float (&v)[4])
+{
+    T x[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) x[i] = (T)v[i];
+    if (n == 4) {
+        Bytes<sizeof(T)> b;
+        __builtin_memcpy(&b, x, sizeof x);
+        *reinterpret_cast<Bytes<sizeof(T)> *>(p) = b;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            if (i < n) p[i] = x[i];
+    }
+}
+
 /* Magnitudes are compared as bit patterns: an infinity or NaN comes out on top, where fmax would drop it. */
 __device__ __forceinline__ uint32_t mag(float v) { return to_bits(v) & 0x7FFFFFFFu; }
 constexpr uint32_t MAG_INF = 0x7F800000u;

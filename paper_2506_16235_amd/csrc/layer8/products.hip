@@ -8,18 +8,11 @@
 
 namespace {
 
-/* What becomes of a sum. */
+/* What becomes of the sums. */
 template <typename T> struct Out {
     T *c;
     uint64_t ldc;
     const float *as, *bs, *bias;
-    __device__ __forceinline__ T value(int sum, float a, uint32_t j) const
-    {
-        float v = (float)sum * a;
-        if (bs) v *= bs[j];
-        if (bias) v += bias[j];
-        return (T)v;
-    }
 };
 
 /* ---------------------------------------------------------------- tiles */
@@ -199,73 +192,130 @@ k_product_large(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, ui
 
 /* ---------------------------------------------------------------- few rows */
 
-/* Up to 16 * MR rows of a against 16 * NC rows of b, k split over the wavefronts in runs of 256 bytes: the weights are read
- * once, each row's run by one wavefront, straight into registers.  The parts meet in LDS. */
-template <typename T, int MR, int NC, int W>
-__global__ void __launch_bounds__(W * 64)
-k_product_few(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t m, uint32_t n, uint32_t k, Out<T> out)
+/* The same for results whose type is looked up once they are there: few, so that it costs nothing, and a third of the kernels. */
+struct AnyOut {
+    void *c;
+    uint64_t ldc;
+    const float *as, *bs, *bias;
+    int type;
+};
+
+/* 16 * MR rows of a against 16 * NC rows of b, k split over W wavefronts in runs of 256 or 512 bytes, straight into registers: a compute unit
+ * reads its rows of b once, and those of a once for all of them.  Bound by memory, so all that matters is that a wavefront's
+ * requests are on their way together.  The parts meet in LDS. */
+template <int MR, int NC, int W>
+__global__ void __launch_bounds__(W * 64, W / 4)
+k_product_few(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t m, uint32_t n, uint32_t k, AnyOut out)
 {
-    __shared__ int sums[MR * 16][NC * 16 + 4];
+    constexpr uint32_t RUN = W == 16 ? 256 : 512;
+    __shared__ int sums[MR * NC][4][64];             /* as a wavefront holds them: additions of 64 lanes meet no bank twice */
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const uint32_t n0 = blockIdx.x * (NC * 16u);
     const uint64_t m0 = (uint64_t)blockIdx.y * (MR * 16u);
     const uint32_t r = lane % 16, part = lane / 16 * 16;
-    for (uint32_t i = threadIdx.x; i < sizeof sums / 4; i += W * 64) (&sums[0][0])[i] = 0;
+    for (uint32_t i = threadIdx.x; i < sizeof sums / 4; i += W * 64) (&sums[0][0][0])[i] = 0;
     v4i acc[MR][NC] = {};
     const int8_t *pa[MR], *pb[NC];
 #pragma unroll
     for (int i = 0; i < MR; i++) pa[i] = a + min<uint64_t>(m0 + i * 16 + r, m - 1) * lda;
 #pragma unroll
     for (int j = 0; j < NC; j++) pb[j] = b + (uint64_t)min(n0 + j * 16 + r, n - 1) * ldb;
-    for (uint32_t k0 = wave * 256u; k0 < k; k0 += W * 256u) {
-        v4i fa[4][MR], fb[4][NC];
+    /* All of a run's rows of b are asked for at once, those of a, which other compute units have read too, half a run at a time. */
+    for (uint32_t k0 = wave * RUN; k0 < k; k0 += W * RUN) {
+        v4i fb[RUN / 64][NC];
 #pragma unroll
-        for (int s = 0; s < 4; s++) {
-            const uint32_t at = k0 + s * 64u + part;
+        for (int s = 0; s < (int)RUN / 64; s++)
 #pragma unroll
-            for (int j = 0; j < NC; j++) fb[s][j] = at < k ? *reinterpret_cast<const v4i *>(pb[j] + at) : v4i{};
+            for (int j = 0; j < NC; j++) {
+                const uint32_t at = k0 + s * 64u + part;
+                fb[s][j] = at < k ? *reinterpret_cast<const v4i *>(pb[j] + at) : v4i{};
+            }
 #pragma unroll
-            for (int i = 0; i < MR; i++)
-                fa[s][i] = at < k && m0 + i * 16 + r < m ? *reinterpret_cast<const v4i *>(pa[i] + at) : v4i{};
-        }
-        if (k0 + 256u > k)
+        for (int h = 0; h < (int)RUN / 64; h += 4) {
+            v4i fa[4][MR];
 #pragma unroll
             for (int s = 0; s < 4; s++)
 #pragma unroll
-                for (int i = 0; i < MR; i++) fa[s][i] = first_bytes(fa[s][i], (int)k - (int)(k0 + s * 64u + part));
+                for (int i = 0; i < MR; i++) {
+                    const uint32_t at = k0 + (h + s) * 64u + part;
+                    fa[s][i] = at < k && m0 + i * 16 + r < m ? *reinterpret_cast<const v4i *>(pa[i] + at) : v4i{};
+                }
+            if (k0 + RUN > k)
 #pragma unroll
-        for (int s = 0; s < 4; s++)
+                for (int s = 0; s < 4; s++)
 #pragma unroll
-            for (int i = 0; i < MR; i++)
+                    for (int i = 0; i < MR; i++) fa[s][i] = first_bytes(fa[s][i], (int)k - (int)(k0 + (h + s) * 64u + part));
 #pragma unroll
-                for (int j = 0; j < NC; j++) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[s][j], fa[s][i], acc[i][j], 0, 0, 0);
+            for (int s = 0; s < 4; s++)
+#pragma unroll
+                for (int i = 0; i < MR; i++)
+#pragma unroll
+                    for (int j = 0; j < NC; j++) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[h + s][j], fa[s][i], acc[i][j], 0, 0, 0);
+        }
     }
     wg_sync();
+    if (wave * RUN < k)
 #pragma unroll
-    for (int i = 0; i < MR; i++)
+        for (int i = 0; i < MR; i++)
 #pragma unroll
-        for (int j = 0; j < NC; j++)
+            for (int j = 0; j < NC; j++)
 #pragma unroll
-            for (int e = 0; e < 4; e++) atomicAdd(&sums[i * 16 + r][j * 16 + lane / 16 * 4 + e], acc[i][j][e]);
+                for (int e = 0; e < 4; e++) atomicAdd(&sums[i * NC + j][e][lane], acc[i][j][e]);
     wg_sync();
-    for (uint32_t i = threadIdx.x; i < MR * NC * 256u; i += W * 64) {
-        const uint32_t row = i / (NC * 16u), col = i % (NC * 16u);
-        if (m0 + row < m && n0 + col < n) out.c[(m0 + row) * out.ldc + n0 + col] = out.value(sums[row][col], out.as[m0 + row], n0 + col);
+    for (uint32_t i = threadIdx.x; i < MR * NC * 64u; i += W * 64) {
+        const uint32_t block = i / 64u, row = block / NC * 16u + lane % 16u, col = n0 + block % NC * 16u + lane / 16u * 4u;
+        if (m0 + row >= m || col >= n) continue;
+        const float as = out.as[m0 + row];
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const uint32_t at = min(col + e, n - 1);
+            v[e] = (float)sums[block][e][lane] * as;
+            if (out.bs) v[e] *= out.bs[at];
+            if (out.bias) v[e] += out.bias[at];
+        }
+        const uint64_t to = (m0 + row) * out.ldc + col;
+        const int have = (int)min(n - col, 4u);
+        if (out.type == NSML_F32) store4(static_cast<float *>(out.c) + to, have, v);
+        else if (out.type == NSML_BF16) store4(static_cast<bf16 *>(out.c) + to, have, v);
+        else store4(static_cast<f16 *>(out.c) + to, have, v);
     }
+}
+
+/* 16 wavefronts where what they hold fits the 128 registers that are left for each, else eight. */
+template <int MR, int NC> int go_few(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t m, uint32_t n, uint32_t k, const AnyOut &out, hipStream_t st)
+{
+    constexpr int W = 16 * (MR + NC) + 4 * MR * NC <= 100 ? 16 : 8;
+    k_product_few<MR, NC, W><<<dim3((n + NC * 16 - 1) / (NC * 16), (uint32_t)((m + MR * 16 - 1) / (MR * 16))), W * 64, 0, st>>>(a, lda, b, ldb, m, n, k, out);
+    return launched();
+}
+template <int MR, typename... A> int few_cols(int nc, A... x)
+{
+    if (nc <= 1) return go_few<MR, 1>(x...);
+    if (nc == 2) return go_few<MR, 2>(x...);
+    if (nc == 3) return go_few<MR, 3>(x...);
+    return go_few<MR, 4>(x...);
+}
+/* As many rows of b to a workgroup as give every compute unit one workgroup. */
+int launch_few(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t m, uint32_t n, uint32_t k, const AnyOut &out, hipStream_t st)
+{
+    const uint64_t groups = (m + 63) / 64 * ((n + 15) / 16);
+    const int nc = (int)((groups + 255) / 256);
+    if (m <= 16) return few_cols<1>(nc, a, lda, b, ldb, m, n, k, out, st);
+    if (m <= 32) return few_cols<2>(nc, a, lda, b, ldb, m, n, k, out, st);
+    if (m <= 48) return few_cols<3>(nc, a, lda, b, ldb, m, n, k, out, st);
+    return few_cols<4>(nc, a, lda, b, ldb, m, n, k, out, st);
+}
+
+/* Up to 64 rows the weights are read once.  Beyond that where there are so few tiles that a long k is better split over wavefronts. */
+bool by_few(uint64_t m, uint32_t n, uint32_t k)
+{
+    return m <= 64 || (m <= 1024 && ((m + 63) / 64) * ((n + 63) / 64) * 4u <= k / 64u);
 }
 
 template <typename T>
 int launch_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t m, uint32_t n, uint32_t k, const Out<T> &out, hipStream_t st)
 {
-    if (m <= 64) {
-        if (m <= 16)
-            k_product_few<T, 1, 1, 16><<<dim3((n + 15) / 16, 1), 1024, 0, st>>>(a, lda, b, ldb, m, n, k, out);
-        else if (m <= 32)
-            k_product_few<T, 2, 2, 8><<<dim3((n + 31) / 32, 1), 512, 0, st>>>(a, lda, b, ldb, m, n, k, out);
-        else
-            k_product_few<T, 4, 2, 8><<<dim3((n + 31) / 32, 1), 512, 0, st>>>(a, lda, b, ldb, m, n, k, out);
-        return launched();
-    }
     const auto tiles = [&](uint64_t s) { return ((m + s - 1) / s) * ((n + s - 1) / s); };
     if (tiles(256) >= (1u << 24)) return NSML_ECAP;
     const uint32_t large = (uint32_t)tiles(256), rest = large % 256u, whole = rest <= 128u ? large - rest : large;
@@ -290,6 +340,7 @@ extern "C" int nsml_q8_matmul(const int8_t *a, uint64_t lda, const float *a_scal
     if (k > NSML_Q8_MAX_COLS || lda > MAX_LD || ldb > MAX_LD) return NSML_ECAP;
     if (m == 0) return NSML_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
+    if (by_few(m, n, k)) return launch_few(a, lda, b, ldb, m, n, k, AnyOut{c, ldc, a_scale, b_scale, bias, type}, st);
     if (type == NSML_F32) return launch_product(a, lda, b, ldb, m, n, k, Out<float>{static_cast<float *>(c), ldc, a_scale, b_scale, bias}, st);
     if (type == NSML_BF16) return launch_product(a, lda, b, ldb, m, n, k, Out<bf16>{static_cast<bf16 *>(c), ldc, a_scale, b_scale, bias}, st);
     return launch_product(a, lda, b, ldb, m, n, k, Out<f16>{static_cast<f16 *>(c), ldc, a_scale, b_scale, bias}, st);

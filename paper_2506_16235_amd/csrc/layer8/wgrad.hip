@@ -27,29 +27,6 @@ __device__ __forceinline__ float left_of(float v)
     return h == v ? 0.0f : v - h;
 }
 
-__device__ __forceinline__ void load4(const float *p, int n, float (&v)[4])
-{
-    if (n == 4) {
-        const auto b = *reinterpret_cast<const Bytes<4> *>(p);
-        __builtin_memcpy(v, &b, 16);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; i++) v[i] = i < n ? p[i] : 0.0f;
-    }
-}
-__device__ __forceinline__ void store4(float *p, int n, const float (&v)[4])
-{
-    if (n == 4) {
-        Bytes<4> b;
-        __builtin_memcpy(&b, v, 16);
-        *reinterpret_cast<Bytes<4> *>(p) = b;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; i++)
-            if (i < n) p[i] = v[i];
-    }
-}
-
 typedef const __attribute__((address_space(1))) uint8_t *Global;
 /* Words at an address of any alignment. */
 typedef uint32_t Loose2 __attribute__((ext_vector_type(2), aligned(1)));
