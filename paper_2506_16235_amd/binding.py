@@ -564,18 +564,30 @@ def _ckpt(name, x, dev, rows=None, cols=None):
     return _CkptArg(at, e, ld, lde), r, c
 
 
+_int8, _uint8, _float32 = torch.int8, torch.uint8, torch.float32
+
+
+def _vec(n: int, dtype, dev, _new=torch.empty_strided) -> torch.Tensor:
+    """A vector (torch.empty takes 0.7 us longer)."""
+    return _new((n,), (1,), dtype=dtype, device=dev)
+
+
+def _mat(rows: int, cols: int, dtype, dev, _new=torch.empty_strided) -> torch.Tensor:
+    return _new((rows, cols), (cols, 1), dtype=dtype, device=dev)
+
+
 def _new_codes(rows: int, cols: int, dev) -> torch.Tensor:
-    ld = (cols + 15) // 16 * 16
-    q = torch.empty((rows, ld), dtype=torch.int8, device=dev)
+    """int8 codes whose rows own their bytes up to the next multiple of 16."""
+    ld = (cols + 15) & ~15
+    q = _mat(rows, ld, _int8, dev)
     return q if ld == cols else q[:, :cols]
 
 
-def _new_q8(rows, cols, dev) -> Q8:
-    return Q8(_new_codes(rows, cols, dev), torch.empty(rows, dtype=torch.float32, device=dev))
-
-
-def _new_ckpt(rows, cols, dev) -> Ckpt8:
-    return Ckpt8(_new_codes(rows, cols, dev), torch.empty((rows, (cols + 31) // 32), dtype=torch.uint8, device=dev))
+def _new_ckpt(rows, cols, dev):
+    """-> (Ckpt8, its argument)."""
+    q, lde = _new_codes(rows, cols, dev), (cols + 31) >> 5
+    e = _mat(rows, lde, _uint8, dev)
+    return Ckpt8(q, e), _CkptArg(q.data_ptr(), e.data_ptr(), (cols + 15) & ~15, lde)
 
 
 def _device_of(name, t) -> torch.device:
@@ -584,16 +596,30 @@ def _device_of(name, t) -> torch.device:
     return t.device
 
 
-def _enqueue(dev, name, *args):
+def _result(name, out, rows, cols, dtype, dev):
+    """-> (matrix to write, address, elements from row to row): the caller's, or a new one."""
+    if out is None:
+        if dtype not in _TYPE:
+            raise ValueError(f"results are float32, bfloat16 or float16, not {dtype}")
+        out = _mat(rows, cols, dtype, dev)
+        return out, out.data_ptr(), cols
+    at, ld, _, _ = _matrix(name, out, dev, None, rows, cols)
+    return out, at, ld
+
+
+_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
+def _enqueue(dev, fn, *args):
     """One call of the library on torch's current stream of the device."""
-    fn = getattr(_lib, name)
-    if torch._C._cuda_getDevice() == dev.index:
-        rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
+    index = dev.index
+    if _current_device() == index:
+        rc = fn(*args, _current_stream(index))
     else:
         with torch.cuda.device(dev):
-            rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
+            rc = fn(*args, _current_stream(index))
     if rc != OK:
-        _check(rc, name)
+        _check(rc, fn.__name__)
 
 
 def q8_rows(x: torch.Tensor, col_scale: Optional[torch.Tensor] = None, out: Optional[Q8] = None) -> Q8:
@@ -602,9 +628,13 @@ def q8_rows(x: torch.Tensor, col_scale: Optional[torch.Tensor] = None, out: Opti
     at, ld, m, k = _matrix("x", x, dev)
     col = _vector("col_scale", col_scale, dev, k)
     if out is None:
-        out = _new_q8(m, k, dev)
-    q, ldq, _, _, s = _rows_of("out", out, dev, m, k)
-    _enqueue(dev, "nsml_q8_rows", at, _TYPE[x.dtype], ld, m, k, col, q, ldq, s)
+        out = Q8(_new_codes(m, k, dev), _vec(m, _float32, dev))
+        q, ldq, s = out.q.data_ptr(), (k + 15) & ~15, out.scale.data_ptr()
+    else:
+        q, ldq, _, _, s = _rows_of("out", out, dev, m, k)
+        if s is None:
+            raise ValueError("out.scale is required")
+    _enqueue(dev, _lib.nsml_q8_rows, at, _TYPE[x.dtype], ld, m, k, col, q, ldq, s)
     return out
 
 
@@ -612,10 +642,8 @@ def q8_values(x: Q8, dtype: torch.dtype = torch.float32, out: Optional[torch.Ten
     """The values that 8-bit rows stand for."""
     dev = _device_of("x.q", x.q)
     q, ldq, m, k, s = _rows_of("x", x, dev)
-    if out is None:
-        out = torch.empty((m, k), dtype=dtype, device=dev)
-    at, ld, _, _ = _matrix("out", out, dev, None, m, k)
-    _enqueue(dev, "nsml_q8_values", q, ldq, s, m, k, at, _TYPE[out.dtype], ld)
+    out, at, ld = _result("out", out, m, k, dtype, dev)
+    _enqueue(dev, _lib.nsml_q8_values, q, ldq, s, m, k, at, _TYPE[out.dtype], ld)
     return out
 
 
@@ -628,10 +656,8 @@ def q8_matmul(a: Q8, b: Q8, dtype: torch.dtype = torch.bfloat16, bias: Optional[
     if sa is None:
         raise ValueError("a.scale is required")
     v = _vector("bias", bias, dev, n)
-    if out is None:
-        out = torch.empty((m, n), dtype=dtype, device=dev)
-    at, ld, _, _ = _matrix("out", out, dev, None, m, n)
-    _enqueue(dev, "nsml_q8_matmul", qa, lda, sa, qb, ldb, sb, v, m, n, k, at, _TYPE[out.dtype], ld)
+    out, at, ld = _result("out", out, m, n, dtype, dev)
+    _enqueue(dev, _lib.nsml_q8_matmul, qa, lda, sa, qb, ldb, sb, v, m, n, k, at, _TYPE[out.dtype], ld)
     return out
 
 
@@ -640,8 +666,10 @@ def ckpt8_pack(x: torch.Tensor, out: Optional[Ckpt8] = None) -> Ckpt8:
     dev = _device_of("x", x)
     at, ld, m, k = _matrix("x", x, dev)
     if out is None:
-        out = _new_ckpt(m, k, dev)
-    _enqueue(dev, "nsml_ckpt8_pack", at, _TYPE[x.dtype], ld, m, k, _ckpt("out", out, dev, m, k)[0])
+        out, arg = _new_ckpt(m, k, dev)
+    else:
+        arg = _ckpt("out", out, dev, m, k)[0]
+    _enqueue(dev, _lib.nsml_ckpt8_pack, at, _TYPE[x.dtype], ld, m, k, arg)
     return out
 
 
@@ -649,10 +677,8 @@ def ckpt8_unpack(x: Ckpt8, dtype: torch.dtype = torch.float32, out: Optional[tor
     """The values that a checkpoint stands for."""
     dev = _device_of("x.q", x.q)
     arg, m, k = _ckpt("x", x, dev)
-    if out is None:
-        out = torch.empty((m, k), dtype=dtype, device=dev)
-    at, ld, _, _ = _matrix("out", out, dev, None, m, k)
-    _enqueue(dev, "nsml_ckpt8_unpack", arg, m, k, at, _TYPE[out.dtype], ld)
+    out, at, ld = _result("out", out, m, k, dtype, dev)
+    _enqueue(dev, _lib.nsml_ckpt8_unpack, arg, m, k, at, _TYPE[out.dtype], ld)
     return out
 
 
@@ -664,9 +690,9 @@ def ckpt8_wgrad(dy: torch.Tensor, x: Ckpt8, col_scale: Optional[torch.Tensor] = 
     at, ld, m, n = _matrix("dy", dy, dev)
     arg, _, k = _ckpt("x", x, dev, m)
     col = _vector("col_scale", col_scale, dev, k)
-    if out is None:
-        out = torch.empty((n, k), dtype=torch.float32, device=dev)
-    w, ldw, _, _ = _matrix("out", out, dev, _F32_ONLY, n, k)
+    if out is not None and out.dtype != _float32:
+        raise ValueError(f"out has dtype {out.dtype}")
+    out, w, ldw = _result("out", out, n, k, _float32, dev)
     base = None
     if add is not None:
         base, lda, _, _ = _matrix("add", add, dev, _F32_ONLY, n, k)
@@ -675,8 +701,8 @@ def ckpt8_wgrad(dy: torch.Tensor, x: Ckpt8, col_scale: Optional[torch.Tensor] = 
         if lda != ldw:
             raise ValueError("add and out must have the same row stride")
     need = _lib.nsml_ckpt8_wgrad_work(m, n, k)
-    work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    _enqueue(dev, "nsml_ckpt8_wgrad", at, _TYPE[dy.dtype], ld, arg, col, m, n, k, base, w, ldw,
+    work = _vec(need, _uint8, dev) if need else None
+    _enqueue(dev, _lib.nsml_ckpt8_wgrad, at, _TYPE[dy.dtype], ld, arg, col, m, n, k, base, w, ldw,
              None if work is None else work.data_ptr(), need)
     return out
 
@@ -689,15 +715,15 @@ def rmsnorm_q8(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, eps: float
     h, r, ldr, ha, ldh = x, None, 0, None, 0
     if residual is not None:
         r, ldr, _, _ = _matrix("residual", residual, dev, x.dtype, m, k)
-        h = torch.empty((m, k), dtype=x.dtype, device=dev)
+        h = _mat(m, k, x.dtype, dev)
         ha, ldh = h.data_ptr(), k
     g = _vector("gamma", gamma, dev, k)
-    y = _new_q8(m, k, dev)
-    rstd = torch.empty(m, dtype=torch.float32, device=dev)
-    xhat = _new_ckpt(m, k, dev) if checkpoint else None
-    _enqueue(dev, "nsml_rmsnorm_q8", at, ld, r, ldr, g, eps, _TYPE[x.dtype], m, k, ha, ldh, y.q.data_ptr(),
-             (k + 15) // 16 * 16, y.scale.data_ptr(), rstd.data_ptr(), None if xhat is None else _ckpt("xhat", xhat, dev)[0])
-    return NormQ8(h, y, rstd, xhat)
+    q, scale = _new_codes(m, k, dev), _vec(m, _float32, dev)
+    rstd = _vec(m, _float32, dev)
+    xhat, arg = _new_ckpt(m, k, dev) if checkpoint else (None, None)
+    _enqueue(dev, _lib.nsml_rmsnorm_q8, at, ld, r, ldr, g, eps, _TYPE[x.dtype], m, k, ha, ldh, q.data_ptr(),
+             (k + 15) & ~15, scale.data_ptr(), rstd.data_ptr(), arg)
+    return NormQ8(h, Q8(q, scale), rstd, xhat)
 
 
 def rmsnorm_backward(dy: torch.Tensor, xhat: Ckpt8, rstd: torch.Tensor, gamma: Optional[torch.Tensor] = None,
@@ -713,15 +739,17 @@ def rmsnorm_backward(dy: torch.Tensor, xhat: Ckpt8, rstd: torch.Tensor, gamma: O
     d, ldd = None, 0
     if dres is not None:
         d, ldd, _, _ = _matrix("dres", dres, dev, dy.dtype, m, k)
-    if out is None:
-        out = torch.empty((m, k), dtype=dy.dtype, device=dev)
-    o, ldo, _, _ = _matrix("out", out, dev, dy.dtype, m, k)
+    if out is not None and out.dtype != dy.dtype:
+        raise ValueError(f"out has dtype {out.dtype}")
+    out, o, ldo = _result("out", out, m, k, dy.dtype, dev)
     if dgamma is None:
-        dgamma = torch.empty(k, dtype=torch.float32, device=dev)
+        dgamma = _vec(k, _float32, dev)
+        dg = dgamma.data_ptr()
+    else:
+        dg = _vector("dgamma", dgamma, dev, k)
     need = _lib.nsml_rmsnorm_backward_work(m, k)
-    work = torch.empty(need, dtype=torch.uint8, device=dev)
-    _enqueue(dev, "nsml_rmsnorm_backward", at, ld, arg, rs, g, d, ldd, _TYPE[dy.dtype], m, k, o, ldo,
-             _vector("dgamma", dgamma, dev, k), work.data_ptr(), need)
+    work = _vec(need, _uint8, dev)
+    _enqueue(dev, _lib.nsml_rmsnorm_backward, at, ld, arg, rs, g, d, ldd, _TYPE[dy.dtype], m, k, o, ldo, dg, work.data_ptr(), need)
     return out, dgamma
 
 
@@ -730,12 +758,11 @@ def swiglu_q8(gate: torch.Tensor, up: torch.Tensor, checkpoint: bool = False) ->
     dev = _device_of("gate", gate)
     g, ldg, m, k = _matrix("gate", gate, dev)
     u, ldu, _, _ = _matrix("up", up, dev, gate.dtype, m, k)
-    a = _new_q8(m, k, dev)
-    held = [_new_ckpt(m, k, dev) for _ in range(3)] if checkpoint else [None] * 3
-    args = [None if c is None else _ckpt("checkpoint", c, dev)[0] for c in held]
-    _enqueue(dev, "nsml_swiglu_q8", g, ldg, u, ldu, _TYPE[gate.dtype], m, k, a.q.data_ptr(), (k + 15) // 16 * 16,
-             a.scale.data_ptr(), *args)
-    return GluQ8(a, *held)
+    q, scale = _new_codes(m, k, dev), _vec(m, _float32, dev)
+    held, args = zip(*(_new_ckpt(m, k, dev) for _ in range(3))) if checkpoint else ((None,) * 3,) * 2
+    _enqueue(dev, _lib.nsml_swiglu_q8, g, ldg, u, ldu, _TYPE[gate.dtype], m, k, q.data_ptr(), (k + 15) & ~15,
+             scale.data_ptr(), *args)
+    return GluQ8(Q8(q, scale), *held)
 
 
 def swiglu_backward(da: torch.Tensor, gate: Ckpt8, up: Ckpt8, dgate: Optional[torch.Tensor] = None,
@@ -744,11 +771,10 @@ def swiglu_backward(da: torch.Tensor, gate: Ckpt8, up: Ckpt8, dgate: Optional[to
     dev = _device_of("da", da)
     at, ld, m, k = _matrix("da", da, dev)
     kg, ku = _ckpt("gate", gate, dev, m, k)[0], _ckpt("up", up, dev, m, k)[0]
-    if dgate is None:
-        dgate = torch.empty((m, k), dtype=da.dtype, device=dev)
-    if dup is None:
-        dup = torch.empty((m, k), dtype=da.dtype, device=dev)
-    g, ldg, _, _ = _matrix("dgate", dgate, dev, da.dtype, m, k)
-    u, ldu, _, _ = _matrix("dup", dup, dev, da.dtype, m, k)
-    _enqueue(dev, "nsml_swiglu_backward", at, ld, kg, ku, _TYPE[da.dtype], m, k, g, ldg, u, ldu)
+    for name, t in (("dgate", dgate), ("dup", dup)):
+        if t is not None and t.dtype != da.dtype:
+            raise ValueError(f"{name} has dtype {t.dtype}")
+    dgate, g, ldg = _result("dgate", dgate, m, k, da.dtype, dev)
+    dup, u, ldu = _result("dup", dup, m, k, da.dtype, dev)
+    _enqueue(dev, _lib.nsml_swiglu_backward, at, ld, kg, ku, _TYPE[da.dtype], m, k, g, ldg, u, ldu)
     return dgate, dup
