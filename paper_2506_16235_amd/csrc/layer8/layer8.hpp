@@ -31,6 +31,26 @@ __device__ __forceinline__ void wg_sync()
 __device__ __forceinline__ float from_bits(uint32_t u) { return __builtin_bit_cast(float, u); }
 __device__ __forceinline__ uint32_t to_bits(float f) { return __builtin_bit_cast(uint32_t, f); }
 
+/* Eight neighbours of a row as they are in memory; the ones from n on are 0 and not read. */
+template <typename T> using Raw = Bytes<sizeof(T) * 2>;
+template <typename T> __device__ __forceinline__ Raw<T> load_raw(const T *p, int n)
+{
+    if (n >= 8) return *reinterpret_cast<const Raw<T> *>(p);
+    T x[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) x[i] = i < n ? p[i] : (T)0.0f;
+    Raw<T> r;
+    __builtin_memcpy(&r, x, sizeof x);
+    return r;
+}
+template <typename T> __device__ __forceinline__ void from_raw(const Raw<T> &r, float (&v)[8])
+{
+    T x[8];
+    __builtin_memcpy(x, &r, sizeof x);
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[i] = (float)x[i];
+}
+
 /* Eight neighbours of a row as binary32; the ones from n on are 0 and not read. */
 template <typename T> __device__ __forceinline__ void load8(const T *p, int n, float (&v)[8])
 {

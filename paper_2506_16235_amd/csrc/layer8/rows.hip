@@ -99,7 +99,9 @@ template <int T, int V, typename OP> int go_rows(const OP &op, uint64_t rows, ui
     k_rows<T, V, OP><<<(uint32_t)(blocks < (1u << 20) ? blocks : 1u << 20), T < 256 ? 256 : T, 0, st>>>(op, rows, cols);
     return launched();
 }
-/* A wavefront holds rows of up to 1024 columns, four wavefronts up to 8192, sixteen up to 32768. */
+/* A wavefront holds rows of up to 1024 columns, four up to 4096, eight up to 16384, sixteen up to 32768: enough threads that their
+ * registers let two workgroups share a compute unit, so that one reads while the other computes (gated activation of 4096 x 11008 with
+ * checkpoints, us: 1024 threads a row 117, 256 126, 512 87). */
 template <typename OP> int launch_rows(const OP &op, uint64_t rows, uint32_t cols, hipStream_t st)
 {
     if (rows == 0) return NSML_OK;
@@ -107,8 +109,9 @@ template <typename OP> int launch_rows(const OP &op, uint64_t rows, uint32_t col
     if (cols <= 1024) return go_rows<64, 2>(op, rows, cols, st);
     if (cols <= 2048) return go_rows<256, 1>(op, rows, cols, st);
     if (cols <= 4096) return go_rows<256, 2>(op, rows, cols, st);
-    if (cols <= 8192) return go_rows<256, 4>(op, rows, cols, st);
-    if (cols <= 16384) return go_rows<1024, 2>(op, rows, cols, st);
+    if (cols <= 8192) return go_rows<512, 2>(op, rows, cols, st);
+    if (cols <= 12288) return go_rows<512, 3>(op, rows, cols, st);
+    if (cols <= 16384) return go_rows<512, 4>(op, rows, cols, st);
     if (cols <= 32768) return go_rows<1024, 4>(op, rows, cols, st);
     return go_rows<1024, 0>(op, rows, cols, st);
 }
@@ -322,37 +325,68 @@ k_norm_back(Mat<const X> dy, Ckpt xhat, const float *rstd, const float *gamma, M
     __shared__ uint32_t sums[2][W > 1 ? W : 1];
     const uint32_t t = threadIdx.x % T;
     const uint64_t first = (uint64_t)blockIdx.x * R + threadIdx.x / T, step = (uint64_t)gridDim.x * R;
-    float g[V][8], dg[V][8];
+    auto at = [&](int i) { return (i * T + t) * 8u; };
+    auto left = [&](int i) { return at(i) < cols ? (int)min(cols - at(i), 8u) : 0; };
+    /* Where registers are short (1024 threads) gamma is read for each row, and the next row is not asked for early. */
+    constexpr bool EARLY = T < 1024;
+    float g[EARLY ? V : 1][8], dg[V][8];
+    auto gammas = [&](int i, float (&v)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] = 1.0f;
+        if (gamma && left(i)) load8(gamma + at(i), left(i), v);
+    };
 #pragma unroll
     for (int i = 0; i < V; i++) {
-        const uint32_t c = (i * T + t) * 8u;
 #pragma unroll
-        for (int j = 0; j < 8; j++) g[i][j] = 1.0f, dg[i][j] = 0.0f;
-        if (gamma && c < cols) load8(gamma + c, (int)min(cols - c, 8u), g[i]);
+        for (int j = 0; j < 8; j++) dg[i][j] = 0.0f;
+        if constexpr (EARLY) gammas(i, g[i]);
     }
+    /* The next row is asked for before this one is worked on. */
+    Raw<X> dn[V], rn[V];
+    uint2 qn[V];
+    uint32_t en[V];
+    float sn;
+    auto ask = [&](uint64_t row) {
+        row = min(row, rows - 1);
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            if (left(i)) {
+                dn[i] = load_raw(dy.at(row, at(i)), left(i));
+                if (dres.p) rn[i] = load_raw(dres.at(row, at(i)), left(i));
+                qn[i] = *reinterpret_cast<const uint2 *>(xhat.q + row * xhat.ldq + at(i));
+                en[i] = xhat.e[row * xhat.lde + at(i) / 32u];
+            }
+        }
+        sn = rstd[row];
+    };
     uint32_t turn = 0;
+    if (EARLY && first < rows) ask(first);
     for (uint64_t row = first; row < rows; row += step, turn ^= 1u) {
+        if (!EARLY) ask(row);
         float d[V][8], x[V][8];
+        Raw<X> res[V];
+        const float r = sn;
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            if (left(i) == 0) continue;
+            from_raw<X>(dn[i], d[i]);
+            codes8(qn[i], x[i]);
+            const float s = ckpt_scale(en[i]);
+#pragma unroll
+            for (int j = 0; j < 8; j++) x[i][j] = at(i) + j < cols ? x[i][j] * s : 0.0f;    /* codes beyond the row are not values */
+            res[i] = rn[i];
+        }
+        if (EARLY) ask(row + step);
         float dot = 0.0f;
 #pragma unroll
         for (int i = 0; i < V; i++) {
-            const uint32_t c = (i * T + t) * 8u;
-            if (c < cols) {
-                load8(dy.at(row, c), (int)min(cols - c, 8u), d[i]);
-                ckpt_load8(xhat, row, c, x[i]);
-            }
-        }
+            if (left(i) == 0) continue;
+            if constexpr (!EARLY) gammas(i, g[0]);
 #pragma unroll
-        for (int i = 0; i < V; i++) {
-            const uint32_t c = (i * T + t) * 8u;
-            if (c < cols) {
-#pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    if (c + j >= cols) x[i][j] = 0.0f;      /* codes beyond the row are not values */
-                    dg[i][j] = __builtin_fmaf(d[i][j], x[i][j], dg[i][j]);
-                    d[i][j] *= g[i][j];
-                    dot = __builtin_fmaf(d[i][j], x[i][j], dot);
-                }
+            for (int j = 0; j < 8; j++) {
+                dg[i][j] = __builtin_fmaf(d[i][j], x[i][j], dg[i][j]);
+                d[i][j] *= g[EARLY ? i : 0][j];
+                dot = __builtin_fmaf(d[i][j], x[i][j], dot);
             }
         }
         dot = from_bits(wave_all(to_bits(dot), sum_of));
@@ -363,25 +397,21 @@ k_norm_back(Mat<const X> dy, Ckpt xhat, const float *rstd, const float *gamma, M
 #pragma unroll
             for (int i = 0; i < W; i++) dot += from_bits(sums[turn][i]);
         }
-        const float mean = dot / (float)cols, r = rstd[row];
+        const float mean = dot / (float)cols;
 #pragma unroll
         for (int i = 0; i < V; i++) {
-            const uint32_t c = (i * T + t) * 8u;
-            if (c < cols) {
-                const int n = (int)min(cols - c, 8u);
-                float v[8] = {};
-                if (dres.p) load8(dres.at(row, c), n, v);
+            if (left(i) == 0) continue;
+            float v[8] = {};
+            if (dres.p) from_raw<X>(res[i], v);
 #pragma unroll
-                for (int j = 0; j < 8; j++) v[j] = __builtin_fmaf(r, d[i][j] - x[i][j] * mean, v[j]);
-                store8(dx.at(row, c), n, v);
-            }
+            for (int j = 0; j < 8; j++) v[j] = __builtin_fmaf(r, d[i][j] - x[i][j] * mean, v[j]);
+            store8(dx.at(row, at(i)), left(i), v);
         }
     }
     if (!part || first >= rows) return;
 #pragma unroll
     for (int i = 0; i < V; i++) {
-        const uint32_t c = (i * T + t) * 8u;
-        if (c < cols) store8(part + first * cols + c, (int)min(cols - c, 8u), dg[i]);
+        if (left(i)) store8(part + first * cols + at(i), left(i), dg[i]);
     }
 }
 
@@ -406,8 +436,8 @@ __global__ void __launch_bounds__(1024) k_norm_sum(const float *part, uint32_t g
 struct BackShape { uint32_t threads, groups; };
 BackShape back_shape(uint64_t rows, uint32_t cols)
 {
-    const uint32_t threads = cols <= 1024 ? 64 : cols <= 8192 ? 256 : 1024;
-    const uint32_t most = threads == 64 ? 2048u : threads == 256 ? 512u : 256u;
+    const uint32_t threads = cols <= 1024 ? 64 : cols <= 2048 ? 256 : cols <= 16384 ? 512 : 1024;
+    const uint32_t most = threads == 64 ? 1024u : threads == 1024 ? 256u : 512u;
     return {threads, (uint32_t)(rows < most ? rows : most)};
 }
 
@@ -423,9 +453,10 @@ template <typename X, typename... A> int launch_back(uint32_t cols, uint32_t gro
     if (cols <= 512) return go_back<X, 64, 1>(groups, st, a...);
     if (cols <= 1024) return go_back<X, 64, 2>(groups, st, a...);
     if (cols <= 2048) return go_back<X, 256, 1>(groups, st, a...);
-    if (cols <= 4096) return go_back<X, 256, 2>(groups, st, a...);
-    if (cols <= 8192) return go_back<X, 256, 4>(groups, st, a...);
-    if (cols <= 16384) return go_back<X, 1024, 2>(groups, st, a...);
+    if (cols <= 4096) return go_back<X, 512, 1>(groups, st, a...);
+    if (cols <= 8192) return go_back<X, 512, 2>(groups, st, a...);
+    if (cols <= 12288) return go_back<X, 512, 3>(groups, st, a...);
+    if (cols <= 16384) return go_back<X, 512, 4>(groups, st, a...);
     return go_back<X, 1024, 4>(groups, st, a...);
 }
 
