@@ -8,6 +8,8 @@
  */
 #include "tiles.hpp"
 
+#include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace {
@@ -20,12 +22,8 @@ template <typename T> constexpr int WORDS = (int)sizeof(T);
 
 /* Upper halves of two binary32 side by side: bfloat16 where the lower halves are 0, else cut off. */
 __device__ __forceinline__ uint32_t upper2(float lo, float hi) { return __builtin_amdgcn_perm(to_bits(hi), to_bits(lo), 0x07060302u); }
-/* What a bfloat16 cut off from v leaves; nothing of an infinity. */
-__device__ __forceinline__ float left_of(float v)
-{
-    const float h = from_bits(to_bits(v) & 0xFFFF0000u);
-    return h == v ? 0.0f : v - h;
-}
+/* What a bfloat16 cut off from v leaves, exactly (of an infinity NaN: what it makes is not finite either way). */
+__device__ __forceinline__ float left_of(float v) { return v - from_bits(to_bits(v) & 0xFFFF0000u); }
 
 typedef const __attribute__((address_space(1))) uint8_t *Global;
 /* Words at an address of any alignment. */
@@ -255,31 +253,47 @@ k_wgrad(Wgrad<T> g)
         }
 }
 
-/* The slices' sums added up in order. */
+/* The slices' sums added up in order, four columns a thread. */
 __global__ void __launch_bounds__(256) k_wgrad_sum(const float *part, const float *col, const float *add, float *dw, uint64_t lddw,
-                                                   uint32_t n, uint32_t k, uint32_t slices)
+                                                   uint32_t n, uint32_t k, uint32_t slices, uint32_t log2l)
 {
-    const uint32_t c = blockIdx.x * 256u + threadIdx.x;
+    const uint32_t c = ((blockIdx.x << log2l) + (threadIdx.x & ((1u << log2l) - 1u))) * 4u, per = 256u >> log2l;
     if (c >= k) return;
-    for (uint32_t row = blockIdx.y; row < n; row += gridDim.y) {
-        float v = 0.0f;
-        for (uint32_t s = 0; s < slices; s++) v += part[((uint64_t)s * n + row) * k + c];
-        if (col) v *= col[c];
-        dw[row * lddw + c] = add ? add[row * lddw + c] + v : v;
+    const int have = (int)min(k - c, 4u);
+    const uint64_t slice = (uint64_t)n * k;
+    float f[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+    if (col) load4(col + c, have, f);
+    for (uint32_t row = blockIdx.y * per + (threadIdx.x >> log2l); row < n; row += gridDim.y * per) {
+        const float *p = part + (uint64_t)row * k + c;
+        float v[4] = {}, old[4] = {};
+        if (add) load4(add + row * lddw + c, have, old);
+#pragma unroll 4
+        for (uint32_t s = 0; s < slices; s++) {
+            float x[4];
+            load4(p + s * slice, have, x);
+#pragma unroll
+            for (int i = 0; i < 4; i++) v[i] += x[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++) v[i] = old[i] + v[i] * f[i];
+        store4(dw + row * lddw + c, have, v);
     }
 }
 
 /* Side of the tiles and number of slices.  Tiles of 256 for bfloat16 where they fill the chip; the parts of the other types take
- * the room that they would need.  Rows are cut into slices where there are fewer tiles than the chip has room for, but no slice is
- * shorter than two stages. */
+ * the room that they would need.  Where there are fewer tiles than the chip has room for (two workgroups a compute unit, one with
+ * parts), the rows are cut into slices: a stage of 64 rows less takes 1.2 us less, a slice more writes and reads 8 bytes more for each
+ * element of dw, at about 4 TB/s, and what is least is taken (1027 x 768 x 768, us for 1, 4 and 8 slices: see the case table). */
 struct Shape { uint32_t side, slices; uint64_t tiles; };
-Shape shape_of(uint64_t rows, uint32_t n, uint32_t k, bool one_part)
+Shape shape_of(uint64_t rows, uint32_t n, uint32_t k, int type)
 {
     const auto tiles = [&](uint64_t s) { return ((n + s - 1) / s) * ((k + s - 1) / s); };
-    const uint32_t side = one_part && tiles(256) >= 192 ? 256 : 128;
-    const uint64_t stages = (rows + 63) / 64;
-    uint64_t s = (side == 256 ? 256 : 512) / tiles(side);
-    if (s > stages / 2) s = stages / 2;
+    const bool one = type == NSML_BF16;
+    const uint32_t side = one && tiles(256) >= 192 ? 256 : 128;
+    const uint64_t stages = (rows + 63) / 64, room = (one && side == 128 ? 512 : 256) / tiles(side);
+    const double stage_us = one ? 1.2 : type == NSML_F16 ? 1.9 : 2.5, slice_us = (double)n * k * 2e-6;
+    uint64_t s = (uint64_t)std::sqrt(stage_us * (double)stages / slice_us);
+    s = std::min(std::min(s, room), stages / 2);
     return {side, s < 2 ? 1u : (uint32_t)s, tiles(side)};
 }
 
@@ -295,7 +309,10 @@ template <typename T> int launch_wgrad(const Wgrad<T> &g, const Shape &s, hipStr
     }
     const int rc = launched();
     if (rc || s.slices == 1) return rc;
-    k_wgrad_sum<<<dim3((g.k + 255u) / 256u, g.n < 65535u ? g.n : 65535u), 256, 0, st>>>(g.part, g.col, g.add, g.dw, g.lddw, g.n, g.k, g.slices);
+    uint32_t log2l = 0;
+    while (log2l < 8u && (4u << log2l) < g.k) log2l++;
+    const uint32_t rows = (g.n + (256u >> log2l) - 1u) / (256u >> log2l);
+    k_wgrad_sum<<<dim3((g.k + (4u << log2l) - 1u) / (4u << log2l), rows < 65535u ? rows : 65535u), 256, 0, st>>>(g.part, g.col, g.add, g.dw, g.lddw, g.n, g.k, g.slices, log2l);
     return launched();
 }
 
@@ -307,7 +324,8 @@ uint64_t nsml_ckpt8_wgrad_work(uint64_t rows, uint32_t n, uint32_t k)
 {
     if (n == 0 || k == 0) return 0;
     /* enough for every type */
-    const uint32_t a = shape_of(rows, n, k, true).slices, b = shape_of(rows, n, k, false).slices, s = a > b ? a : b;
+    uint32_t s = 1;
+    for (int type : {NSML_F32, NSML_BF16, NSML_F16}) s = std::max(s, shape_of(rows, n, k, type).slices);
     return s > 1 ? (uint64_t)s * n * k * 4u : 0u;
 }
 
@@ -320,7 +338,7 @@ int nsml_ckpt8_wgrad(const void *dy, int type, uint64_t lddy, const nsml_ckpt8 *
         return NSML_EINVAL;
     const uint64_t need = nsml_ckpt8_wgrad_work(rows, n, k);
     if (need && (!work || !at_multiple(work, 16) || work_bytes < need)) return NSML_EINVAL;
-    const Shape s = shape_of(rows, n, k, type == NSML_BF16);
+    const Shape s = shape_of(rows, n, k, type);
     if (s.tiles >= (1u << 24) || (rows && (lddy >= MAX_LD || x->ldq >= MAX_LD || x->lde >= MAX_LD))) return NSML_ECAP;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const auto go = [&](auto v) {
