@@ -638,6 +638,15 @@ def q8_rows(x: torch.Tensor, col_scale: Optional[torch.Tensor] = None, out: Opti
     return out
 
 
+def q8_transposed(w: Q8) -> Q8:
+    """The codes of w the other way round, without scales: what the gradient of the data is multiplied by,
+    q8_matmul(q8_rows(dc, col_scale=w.scale), q8_transposed(w)).  A layout to make once per update of the weights."""
+    _, _, n, k, _ = _rows_of("w", w, _device_of("w.q", w.q))
+    out = _new_codes(k, n, w.q.device)
+    out.copy_(w.q.t())
+    return Q8(out, None)
+
+
 def q8_values(x: Q8, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The values that 8-bit rows stand for."""
     dev = _device_of("x.q", x.q)

@@ -513,6 +513,7 @@ def test_no_rows_at_all():
     assert nsml.ckpt8_unpack(nsml.ckpt8_pack(x)).shape == (0, 40)
     o = nsml.rmsnorm_q8(x, torch.ones(40, device=DEV), residual=x, checkpoint=True)
     w = nsml.q8_rows(torch.ones(24, 40, device=DEV))
+    assert nsml.q8_transposed(w).q.shape == (40, 24)
     assert nsml.q8_matmul(o.y, w).shape == (0, 24)
     s = nsml.swiglu_q8(x, x, checkpoint=True)
     assert nsml.swiglu_backward(x, s.gate, s.up)[0].shape == (0, 40)
