@@ -1,10 +1,11 @@
 /*
  * Tiles in LDS for the matrix instructions, shared by the products and the weight gradient.
  *
- * A tile's row is 128 bytes of the summed dimension (128 codes, or 64 bfloat16) in eight chunks of 16 bytes.  Two neighbouring
- * rows share 256 bytes, all the banks of LDS once, and their sixteen chunks lie there in an order that is another one for each
- * of 16 neighbouring pairs, so that the same chunk of 32 rows, which is what a matrix instruction reads, meets every bank equally
- * often.  Rows 32 apart have the same order: one address per operand and chunk does for all of a wavefront's blocks.
+ * The products' rows (spot) are 64 bytes of the summed dimension, the weight gradient's (place) 128.  Measured here for accesses of 16
+ * bytes per lane: a read takes 16 lanes a cycle (lanes 0-3, 12-15, 20-23 and 24-27, and so on) and a write eight neighbouring
+ * ones, over 256 and 128 bytes of banks.  So the chunks of 16 bytes lie within 256 bytes in an order that differs from pair (place) or
+ * four (spot) of rows to the next, such that reads of the same chunk of 32 rows, and writes of the same chunk of
+ * consecutive rows, meet no bank twice.  Rows 32 apart have the same order: one address per operand does for all blocks.
  */
 #ifndef NSML_LAYER8_TILES_HPP
 #define NSML_LAYER8_TILES_HPP
@@ -23,7 +24,7 @@ constexpr uint64_t MAX_LD = 1u << 22;
 
 __device__ __forceinline__ uint32_t place(uint32_t row, uint32_t chunk)
 {
-    return row / 2u * 256u + ((((row % 2u) * 8u + chunk) ^ (row / 2u % 16u)) * 16u);
+    return row / 2u * 256u + ((row % 2u * 12u ^ chunk ^ row / 2u % 8u) * 16u);
 }
 constexpr uint32_t BLOCK = 32 * 128;                 /* bytes from one block of 32 rows to the next */
 
