@@ -146,14 +146,15 @@ __device__ __forceinline__ uint32_t ckpt_exp(uint32_t m)
     return m >= MAG_INF ? 255u : (uint32_t)(e < 1 ? 1 : e);
 }
 __device__ __forceinline__ float ckpt_scale(uint32_t e) { return from_bits(e << 23); }      /* 2^(e - 127); e = 255: infinity */
-/* Codes of eight values of a block: multiplied by 2^(127 - e), which is exact wherever the code is not 0. */
+/* Codes of eight values of a block: held to 127 steps, divided by the step (exact: powers of two) and rounded, the last two in one
+ * instruction whose sum has the code in its low byte. */
 __device__ __forceinline__ uint2 ckpt_codes8(const float (&x)[8], uint32_t e)
 {
     if (e == 255u) return make_uint2(0, 0);
-    const float inv = from_bits((254u - e) << 23);
+    const float inv = from_bits((254u - e) << 23), most = 127.0f * ckpt_scale(e);
     uint32_t c[8];
 #pragma unroll
-    for (int i = 0; i < 8; i++) c[i] = code(__builtin_amdgcn_fmed3f(x[i] * inv, -127.0f, 127.0f));
+    for (int i = 0; i < 8; i++) c[i] = to_bits(__builtin_fmaf(__builtin_amdgcn_fmed3f(x[i], -most, most), inv, 12582912.0f));
     return make_uint2(pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7]));
 }
 __device__ __forceinline__ void codes8(uint2 w, float (&v)[8])
