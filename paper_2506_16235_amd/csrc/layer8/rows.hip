@@ -33,7 +33,7 @@ __device__ __forceinline__ uint32_t sum_of(uint32_t a, uint32_t b) { return to_b
 
 /* T threads hold a row, V times eight neighbours each; V == 0: rows wider than registers hold are read twice.
  * OP: load() gives the values to code and adds to the row's sum, done() gets the sum and the row's code,
- * store() writes beside the codes. */
+ * store() writes beside the codes.  SHORT: two times eight per thread at most. */
 template <int T, int V, typename OP>
 __global__ void __launch_bounds__(T < 256 ? 256 : T) k_rows(OP op, uint64_t rows, uint32_t cols)
 {
@@ -99,9 +99,10 @@ template <int T, int V, typename OP> int go_rows(const OP &op, uint64_t rows, ui
     k_rows<T, V, OP><<<(uint32_t)(blocks < (1u << 20) ? blocks : 1u << 20), T < 256 ? 256 : T, 0, st>>>(op, rows, cols);
     return launched();
 }
-/* A wavefront holds rows of up to 1024 columns, four up to 4096, eight up to 16384, sixteen up to 32768: enough threads that their
- * registers let two workgroups share a compute unit, so that one reads while the other computes (gated activation of 4096 x 11008 with
- * checkpoints, us: 1024 threads a row 117, 256 126, 512 87). */
+/* A wavefront holds rows of up to 1024 columns, four up to 4096, eight up to 8192; beyond that as many as the operator's registers make
+ * best: with few registers each, workgroups share a compute unit and one reads while the other computes, with more, less of them wait
+ * at a row's barrier (rows of 11008, us for 1024 x 2, 768 x 2, 512 x 3, 256 x 6 threads times eights: gated activation of 4096 with
+ * checkpoints 117, 77, 86, 126; norm of 8192 with its checkpoint 211 (768), 175 (512), 200 (256); codes alone 61, 49, 45, 50). */
 template <typename OP> int launch_rows(const OP &op, uint64_t rows, uint32_t cols, hipStream_t st)
 {
     if (rows == 0) return NSML_OK;
@@ -110,14 +111,14 @@ template <typename OP> int launch_rows(const OP &op, uint64_t rows, uint32_t col
     if (cols <= 2048) return go_rows<256, 1>(op, rows, cols, st);
     if (cols <= 4096) return go_rows<256, 2>(op, rows, cols, st);
     if (cols <= 8192) return go_rows<512, 2>(op, rows, cols, st);
-    if (cols <= 12288) return go_rows<512, 3>(op, rows, cols, st);
-    if (cols <= 16384) return go_rows<512, 4>(op, rows, cols, st);
+    if (cols <= 12288) return go_rows<OP::SHORT ? 768 : 512, OP::SHORT ? 2 : 3>(op, rows, cols, st);
+    if (cols <= 16384) return go_rows<OP::SHORT ? 1024 : 512, OP::SHORT ? 2 : 4>(op, rows, cols, st);
     if (cols <= 32768) return go_rows<1024, 4>(op, rows, cols, st);
     return go_rows<1024, 0>(op, rows, cols, st);
 }
 
 template <typename T> struct OpRows {
-    static constexpr bool SUMS = false;
+    static constexpr bool SUMS = false, SHORT = false;
     struct Reg { float t[8]; };
     Mat<const T> x;
     const float *col;
@@ -144,7 +145,7 @@ template <typename T> struct OpRows {
 /* The norm: codes are those of gamma * h, so that they wait for the absmax alone; the mean of h^2, which comes out of
  * the same reduction, goes into the scale. */
 template <typename T> struct OpNorm {
-    static constexpr bool SUMS = true;
+    static constexpr bool SUMS = true, SHORT = false;
     struct Reg { float t[8], h[8]; };
     Mat<const T> x, res;
     const float *gamma;
@@ -203,7 +204,7 @@ __device__ __forceinline__ float sigmoid(float x)
 }
 
 template <typename T> struct OpGlu {
-    static constexpr bool SUMS = false;
+    static constexpr bool SUMS = false, SHORT = true;
     struct Reg { float t[8]; };
     Mat<const T> gate, up;
     Mat<int8_t> q;
