@@ -50,6 +50,10 @@ __device__ __forceinline__ void product_tile(uint8_t *lds, uint64_t m0, uint32_t
         chunk[l] = at % 4u * 16u;
         off[l] = row * (uint32_t)(l < LA ? lda : ldb);
     }
+    /* The scales are asked for before they are needed, those of a before anything else. */
+    float as[TM];
+#pragma unroll
+    for (int i = 0; i < TM; i++) as[i] = out.as[m0 + min(wm + i * 32 + lane % 32, rows_a - 1)];
     const uint32_t stages = (k + DEPTH - 1) / DEPTH;
     auto request = [&](uint32_t stage, uint32_t ring, int l) {
         const uint32_t k0 = min(stage, stages - 1u) * DEPTH;
@@ -114,24 +118,23 @@ __device__ __forceinline__ void product_tile(uint8_t *lds, uint64_t m0, uint32_t
         there = here;
         here = next;
     }
+    float bs[TN][16];
+#pragma unroll
+    for (int j = 0; j < TN; j++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) bs[j][e] = out.bs ? out.bs[min(n0 + wn + j * 32 + acc_row(e, lane), n - 1)] : 1.0f;
     loads_sync<0>();
     /* Out through LDS, 32 rows of a wavefront's part at a time, so that lines are written whole. */
     constexpr int COLS = TN * 32, PITCH = COLS * (int)sizeof(T) + 16, LANES = COLS * (int)sizeof(T) / 16, PER = 16 / (int)sizeof(T);
     static_assert(32 * PITCH * W <= RING * STAGE, "room for every wavefront");
     uint8_t *mine = lds + wave * (32 * PITCH);
-    float bs[TN][16], bias[TN][16];
+    float bias[TN][16];
 #pragma unroll
     for (int j = 0; j < TN; j++)
 #pragma unroll
-        for (int e = 0; e < 16; e++) {
-            const uint32_t col = min(n0 + wn + j * 32 + acc_row(e, lane), n - 1);
-            bs[j][e] = out.bs ? out.bs[col] : 1.0f;
-            bias[j][e] = out.bias ? out.bias[col] : 0.0f;
-        }
+        for (int e = 0; e < 16; e++) bias[j][e] = out.bias ? out.bias[min(n0 + wn + j * 32 + acc_row(e, lane), n - 1)] : 0.0f;
 #pragma unroll
     for (int i = 0; i < TM; i++) {
-        const uint32_t row = wm + i * 32 + lane % 32;
-        const float as = out.as[m0 + min(row, rows_a - 1)];
 #pragma unroll
         for (int j = 0; j < TN; j++)
 #pragma unroll
@@ -139,7 +142,7 @@ __device__ __forceinline__ void product_tile(uint8_t *lds, uint64_t m0, uint32_t
                 const uint32_t col = j * 32 + q * 8 + lane / 32 * 4;
                 T v[4];
 #pragma unroll
-                for (int e = 0; e < 4; e++) v[e] = (T)((float)acc[i][j][q * 4 + e] * as * bs[j][q * 4 + e] + bias[j][q * 4 + e]);
+                for (int e = 0; e < 4; e++) v[e] = (T)((float)acc[i][j][q * 4 + e] * as[i] * bs[j][q * 4 + e] + bias[j][q * 4 + e]);
                 __builtin_memcpy(__builtin_assume_aligned(mine + lane % 32 * PITCH + col * sizeof(T), sizeof v), v, sizeof v);
             }
 #pragma unroll
