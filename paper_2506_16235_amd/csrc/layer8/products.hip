@@ -25,8 +25,9 @@ __device__ __forceinline__ uint32_t spot(uint32_t row, uint32_t chunk) { return 
 /* A tile of BM x BN by WM x WN wavefronts.  Stages go from memory straight into a ring of places in LDS, all but one ahead; a wavefront's
  * requests are spread between its matrix instructions, as one that waits to make a request multiplies nothing.  The matrix instructions of
  * a stage's second half run while the next stage's first half is read from LDS: the barrier between stages stands before them,
- * when all of the stage is in registers. */
-template <typename T, int BM, int BN, int WM, int WN, int RING>
+ * when all of the stage is in registers.  PAST: results go past the caches, where the operands are read from (8192 x 4096 x 4096: 137 us
+ * and 130). */
+template <typename T, int BM, int BN, int WM, int WN, int RING, bool PAST>
 __device__ __forceinline__ void product_tile(uint8_t *lds, uint64_t m0, uint32_t n0, const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb,
                                              uint64_t m, uint32_t n, uint32_t k, const Out<T> &out)
 {
@@ -153,9 +154,10 @@ __device__ __forceinline__ void product_tile(uint8_t *lds, uint64_t m0, uint32_t
             if (to < rows_a) {
                 T *p = out.c + (m0 + to) * out.ldc + n0 + at;
                 if (at + PER <= rows_b) {
-                    Bytes<4> x;
+                    Loose4 x;
                     __builtin_memcpy(&x, v, 16);
-                    *reinterpret_cast<Bytes<4> *>(p) = x;
+                    if (PAST) __builtin_nontemporal_store(x, reinterpret_cast<Loose4 *>(p));
+                    else *reinterpret_cast<Loose4 *>(p) = x;
                 } else {
 #pragma unroll
                     for (int e = 0; e < PER; e++)
@@ -172,7 +174,7 @@ k_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t
 {
     __shared__ __align__(16) uint8_t lds[RING * 2 * SIDE * DEPTH];
     const Tile tile = tile_of(blockIdx.x, (uint32_t)((m + SIDE - 1) / SIDE), (n + SIDE - 1) / SIDE);
-    product_tile<T, SIDE, SIDE, 2, 2, RING>(lds, (uint64_t)tile.row * SIDE, tile.col * SIDE, a, lda, b, ldb, m, n, k, out);
+    product_tile<T, SIDE, SIDE, 2, 2, RING, false>(lds, (uint64_t)tile.row * SIDE, tile.col * SIDE, a, lda, b, ldb, m, n, k, out);
 }
 
 /* Tiles of 256 x 256, one workgroup a compute unit.  Those from `whole` on, which would leave half of the chip or more without work
@@ -185,11 +187,11 @@ k_product_large(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, ui
     const uint32_t id = blockIdx.x, rows = (uint32_t)((m + 255) / 256), cols = (n + 255) / 256;
     if (id < whole) {
         const Tile tile = tile_of(id, rows, cols);
-        product_tile<T, 256, 256, 2, 4, 4>(lds, (uint64_t)tile.row * 256, tile.col * 256u, a, lda, b, ldb, m, n, k, out);
+        product_tile<T, 256, 256, 2, 4, 4, true>(lds, (uint64_t)tile.row * 256, tile.col * 256u, a, lda, b, ldb, m, n, k, out);
     } else {
         const Tile tile = tile_of(whole + (id - whole) / 2u, rows, cols);
         const uint64_t m0 = (uint64_t)tile.row * 256 + (id - whole) % 2u * 128u;
-        if (m0 < m) product_tile<T, 128, 256, 2, 4, 4>(lds, m0, tile.col * 256u, a, lda, b, ldb, m, n, k, out);
+        if (m0 < m) product_tile<T, 128, 256, 2, 4, 4, true>(lds, m0, tile.col * 256u, a, lda, b, ldb, m, n, k, out);
     }
 }
 

@@ -19,6 +19,10 @@ typedef int v16i __attribute__((ext_vector_type(16)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 
+/* Words at an address of any alignment. */
+typedef uint32_t Loose2 __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t Loose4 __attribute__((ext_vector_type(4), aligned(1)));
+
 /* Longest row stride: the rows of a tile lie within 32 bits of its first. */
 constexpr uint64_t MAX_LD = 1u << 22;
 
@@ -58,13 +62,13 @@ __device__ __forceinline__ v4i first_bytes(v4i v, int n)
 }
 
 /* Which tile a workgroup takes.  Workgroups go round the eight dies; each die gets a run of neighbouring tiles, in bands of
- * eight tile rows, so that what its workgroups read at the same time is shared in its cache. */
+ * four tile rows, so that what its 32 workgroups read at the same time is shared in its cache (bands of 8 and 16: 1 and 2 % more time). */
 struct Tile { uint32_t row, col; };
 __device__ __forceinline__ Tile tile_of(uint32_t id, uint32_t rows, uint32_t cols)
 {
     const uint32_t total = rows * cols, per = total / 8u, more = total % 8u, die = id % 8u;
     const uint32_t i = die * per + min(die, more) + id / 8u;
-    const uint32_t band = i / (8u * cols), first = band * 8u, high = min(rows - first, 8u), in = i - band * 8u * cols;
+    const uint32_t band = i / (4u * cols), first = band * 4u, high = min(rows - first, 4u), in = i - band * 4u * cols;
     return {first + in % high, in / high};
 }
 
