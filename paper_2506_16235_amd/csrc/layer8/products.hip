@@ -13,6 +13,7 @@ template <typename T> struct Out {
     T *c;
     uint64_t ldc;
     const float *as, *bs, *bias;
+    bool past;                   /* past the caches */
 };
 
 /* ---------------------------------------------------------------- tiles */
@@ -25,9 +26,8 @@ __device__ __forceinline__ uint32_t spot(uint32_t row, uint32_t chunk) { return 
 /* A tile of BM x BN by WM x WN wavefronts.  Stages go from memory straight into a ring of places in LDS, all but one ahead; a wavefront's
  * requests are spread between its matrix instructions, as one that waits to make a request multiplies nothing.  The matrix instructions of
  * a stage's second half run while the next stage's first half is read from LDS: the barrier between stages stands before them,
- * when all of the stage is in registers.  PAST: results go past the caches, where the operands are read from (8192 x 4096 x 4096: 137 us
- * and 130). */
-template <typename T, int BM, int BN, int WM, int WN, int RING, bool PAST>
+ * when all of the stage is in registers. */
+template <typename T, int BM, int BN, int WM, int WN, int RING>
 __device__ __forceinline__ void product_tile(uint8_t *lds, uint64_t m0, uint32_t n0, const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb,
                                              uint64_t m, uint32_t n, uint32_t k, const Out<T> &out)
 {
@@ -156,7 +156,7 @@ __device__ __forceinline__ void product_tile(uint8_t *lds, uint64_t m0, uint32_t
                 if (at + PER <= rows_b) {
                     Loose4 x;
                     __builtin_memcpy(&x, v, 16);
-                    if (PAST) __builtin_nontemporal_store(x, reinterpret_cast<Loose4 *>(p));
+                    if (out.past) __builtin_nontemporal_store(x, reinterpret_cast<Loose4 *>(p));
                     else *reinterpret_cast<Loose4 *>(p) = x;
                 } else {
 #pragma unroll
@@ -174,7 +174,7 @@ k_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t
 {
     __shared__ __align__(16) uint8_t lds[RING * 2 * SIDE * DEPTH];
     const Tile tile = tile_of(blockIdx.x, (uint32_t)((m + SIDE - 1) / SIDE), (n + SIDE - 1) / SIDE);
-    product_tile<T, SIDE, SIDE, 2, 2, RING, false>(lds, (uint64_t)tile.row * SIDE, tile.col * SIDE, a, lda, b, ldb, m, n, k, out);
+    product_tile<T, SIDE, SIDE, 2, 2, RING>(lds, (uint64_t)tile.row * SIDE, tile.col * SIDE, a, lda, b, ldb, m, n, k, out);
 }
 
 /* Tiles of 256 x 256, one workgroup a compute unit.  Those from `whole` on, which would leave half of the chip or more without work
@@ -187,11 +187,11 @@ k_product_large(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, ui
     const uint32_t id = blockIdx.x, rows = (uint32_t)((m + 255) / 256), cols = (n + 255) / 256;
     if (id < whole) {
         const Tile tile = tile_of(id, rows, cols);
-        product_tile<T, 256, 256, 2, 4, 4, true>(lds, (uint64_t)tile.row * 256, tile.col * 256u, a, lda, b, ldb, m, n, k, out);
+        product_tile<T, 256, 256, 2, 4, 4>(lds, (uint64_t)tile.row * 256, tile.col * 256u, a, lda, b, ldb, m, n, k, out);
     } else {
         const Tile tile = tile_of(whole + (id - whole) / 2u, rows, cols);
         const uint64_t m0 = (uint64_t)tile.row * 256 + (id - whole) % 2u * 128u;
-        if (m0 < m) product_tile<T, 128, 256, 2, 4, 4, true>(lds, m0, tile.col * 256u, a, lda, b, ldb, m, n, k, out);
+        if (m0 < m) product_tile<T, 128, 256, 2, 4, 4>(lds, m0, tile.col * 256u, a, lda, b, ldb, m, n, k, out);
     }
 }
 
@@ -319,11 +319,14 @@ bool by_few(uint64_t m, uint32_t n, uint32_t k)
 }
 
 template <typename T>
-int launch_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t m, uint32_t n, uint32_t k, const Out<T> &out, hipStream_t st)
+int launch_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t m, uint32_t n, uint32_t k, Out<T> out, hipStream_t st)
 {
     const auto tiles = [&](uint64_t s) { return ((m + s - 1) / s) * ((n + s - 1) / s); };
     if (tiles(256) >= (1u << 24)) return NSML_ECAP;
     const uint32_t large = (uint32_t)tiles(256), rest = large % 256u, whole = rest <= 128u ? large - rest : large;
+    /* Large results go past the caches, where the operands are read from, if their rows are whole lines: 8192 x 11008 x 1024 131 -> 124 us,
+     * but 8192 x 5001 x 512 40 -> 56. */
+    out.past = large >= 96 && whole_lines(out.c, out.ldc * sizeof(T));
     if (large >= 96)
         k_product_large<T><<<whole + (large - whole) * 2u, 512, 0, st>>>(a, lda, b, ldb, m, n, k, out, whole);
     else if (tiles(128) >= 256)
@@ -346,7 +349,7 @@ extern "C" int nsml_q8_matmul(const int8_t *a, uint64_t lda, const float *a_scal
     if (m == 0) return NSML_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (by_few(m, n, k)) return launch_few(a, lda, b, ldb, m, n, k, AnyOut{c, ldc, a_scale, b_scale, bias, type}, st);
-    if (type == NSML_F32) return launch_product(a, lda, b, ldb, m, n, k, Out<float>{static_cast<float *>(c), ldc, a_scale, b_scale, bias}, st);
-    if (type == NSML_BF16) return launch_product(a, lda, b, ldb, m, n, k, Out<bf16>{static_cast<bf16 *>(c), ldc, a_scale, b_scale, bias}, st);
-    return launch_product(a, lda, b, ldb, m, n, k, Out<f16>{static_cast<f16 *>(c), ldc, a_scale, b_scale, bias}, st);
+    if (type == NSML_F32) return launch_product(a, lda, b, ldb, m, n, k, Out<float>{static_cast<float *>(c), ldc, a_scale, b_scale, bias, false}, st);
+    if (type == NSML_BF16) return launch_product(a, lda, b, ldb, m, n, k, Out<bf16>{static_cast<bf16 *>(c), ldc, a_scale, b_scale, bias, false}, st);
+    return launch_product(a, lda, b, ldb, m, n, k, Out<f16>{static_cast<f16 *>(c), ldc, a_scale, b_scale, bias, false}, st);
 }

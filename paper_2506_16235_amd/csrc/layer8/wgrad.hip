@@ -35,6 +35,7 @@ template <typename T> struct Wgrad {
     float *dw, *part;            /* part: sums of the slices when there is more than one */
     uint64_t lddw, rows;
     uint32_t n, k, slices;
+    bool past;                   /* dw past the caches */
 };
 
 /* A tile of BN x BK of dw by WM x WN wavefronts, one slice of the rows, 64 rows to a stage.  Every thread brings eight rows of four
@@ -246,7 +247,7 @@ k_wgrad(Wgrad<T> g)
             if (add) load4(add + row * ld + c, have, old);
 #pragma unroll
             for (int j = 0; j < 4; j++) v[j] = old[j] + acc[i][j][r] * s[j];
-            if (BN == 256 && have == 4) {            /* past the caches, where dy and x are read from (11008 x 4096: 764 us and 728) */
+            if (g.past && have == 4) {
                 Loose4 x;
                 __builtin_memcpy(&x, v, 16);
                 __builtin_nontemporal_store(x, reinterpret_cast<Loose4 *>(to_dw + row * ld + c));
@@ -344,9 +345,12 @@ int nsml_ckpt8_wgrad(const void *dy, int type, uint64_t lddy, const nsml_ckpt8 *
     const Shape s = shape_of(rows, n, k, type);
     if (s.tiles >= (1u << 24) || (rows && (lddy >= MAX_LD || x->ldq >= MAX_LD || x->lde >= MAX_LD))) return NSML_ECAP;
     hipStream_t st = static_cast<hipStream_t>(stream);
+    /* Large results past the caches, where dy and x are read from, if their rows are whole lines (8192 x 11008 x 4096: 764 -> 728 us; see
+     * the products for rows that are not). */
+    const bool past = s.side == 256 && s.slices == 1 && whole_lines(dw, lddw * 4u);
     const auto go = [&](auto v) {
         using T = decltype(v);
-        return launch_wgrad(Wgrad<T>{mat<T>(dy, lddy), ckpt_of(x), col_scale, add, dw, static_cast<float *>(work), lddw, rows, n, k, s.slices}, s, st);
+        return launch_wgrad(Wgrad<T>{mat<T>(dy, lddy), ckpt_of(x), col_scale, add, dw, static_cast<float *>(work), lddw, rows, n, k, s.slices, past}, s, st);
     };
     if (type == NSML_F32) return go(float{});
     if (type == NSML_BF16) return go(bf16{});
