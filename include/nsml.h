@@ -295,7 +295,8 @@ int nsml_last_l2norm(nsml_ctx *ctx, double *total, double *per_bucket);
  *   code matrices   16-byte aligned, ld a multiple of 16; the bytes of a row up to the next multiple of 16
  *             belong to it (their contents are never used as values, and may be overwritten)
  * NSML_EINVAL: a null pointer, an unknown type, cols == 0, ld < cols, a code matrix or pointer that is not aligned
- * as above; NSML_ECAP: cols beyond the limit named; NSML_EHIP: the launch failed.  Buffers of one call
+ * as above; NSML_ECAP: cols beyond the limit named (2^31 - 256 if none is), an ld of a product's or weight gradient's
+ * operand beyond 2^22; NSML_EHIP: the launch failed.  Buffers of one call
  * must not overlap where one of them is written, unless said otherwise. */
 
 #define NSML_F32  0

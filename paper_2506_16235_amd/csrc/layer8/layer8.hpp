@@ -212,6 +212,7 @@ __device__ __forceinline__ void ckpt_store8(const Ckpt &k, uint64_t row, uint32_
 
 /* ---------------------------------------------------------------- host */
 
+constexpr uint32_t MAX_COLS = 0x7FFFFF00u;          /* so that column numbers rounded up to a tile stay below 2^31 */
 inline bool at_multiple(const void *p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 inline bool whole_lines(const void *p, uint64_t row_bytes) { return at_multiple(p, 128) && row_bytes % 128 == 0; }
 inline uint32_t type_bytes(int type) { return type == NSML_F32 ? 4u : 2u; }

@@ -294,28 +294,34 @@ template <int MR, int NC> int go_few(const int8_t *a, uint64_t lda, const int8_t
     k_product_few<MR, NC, W><<<dim3((n + NC * 16 - 1) / (NC * 16), (uint32_t)((m + MR * 16 - 1) / (MR * 16))), W * 64, 0, st>>>(a, lda, b, ldb, m, n, k, out);
     return launched();
 }
-template <int MR, typename... A> int few_cols(int nc, A... x)
+/* As many rows of b to a workgroup as give every compute unit one workgroup (us for 16, 32, 48 and 64 rows, k = 4096: 1 x 4096 6.3, 7.4, 9.1, 10.8;
+ * 48 x 4096 11.5, 12.9, 15.5, 17.5; 1 x 11008 13.3, 15.4, 13.1, 15.2).  More than 32 rows of a come here only where 32 of b do. */
+template <int MR, typename... A> int few_cols(uint64_t nc, A... x)
 {
     if (nc <= 1) return go_few<MR, 1>(x...);
-    if (nc == 2) return go_few<MR, 2>(x...);
-    if (nc == 3) return go_few<MR, 3>(x...);
-    return go_few<MR, 4>(x...);
+    if constexpr (MR <= 2) {
+        if (nc == 3) return go_few<MR, 3>(x...);
+        if (nc > 3) return go_few<MR, 4>(x...);
+    }
+    return go_few<MR, 2>(x...);
 }
-/* As many rows of b to a workgroup as give every compute unit one workgroup. */
 int launch_few(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t m, uint32_t n, uint32_t k, const AnyOut &out, hipStream_t st)
 {
-    const uint64_t groups = (m + 63) / 64 * ((n + 15) / 16);
-    const int nc = (int)((groups + 255) / 256);
+    const uint64_t groups = (m + 63) / 64 * ((n + 15) / 16), nc = (groups + 255) / 256;
     if (m <= 16) return few_cols<1>(nc, a, lda, b, ldb, m, n, k, out, st);
     if (m <= 32) return few_cols<2>(nc, a, lda, b, ldb, m, n, k, out, st);
     if (m <= 48) return few_cols<3>(nc, a, lda, b, ldb, m, n, k, out, st);
     return few_cols<4>(nc, a, lda, b, ldb, m, n, k, out, st);
 }
 
-/* Up to 64 rows the weights are read once.  Beyond that where there are so few tiles that a long k is better split over wavefronts. */
-bool by_few(uint64_t m, uint32_t n, uint32_t k)
+/* Whether k is split over the wavefronts of a workgroup.  Up to 64 rows, unless there are so many rows of b that tiles fill the chip and
+ * their ring in LDS keeps more on its way (us, split and in tiles; k = 4096: 1 x 11008 14, 15; 48 x 11008 20, 18; 64 x 4096 14, 14;
+ * 16 x 32000 36, 33; 64 x 32000 65, 37).  Beyond that where there are few tiles (512 x 512 x 4096 12, 14; 128 x 768 x 11008 27, 32; 128 x
+ * 4096 x 4096 15, 14; 1000 x 1543 x 1024 21, 8). */
+bool by_few(uint64_t m, uint32_t n)
 {
-    return m <= 64 || (m <= 1024 && ((m + 63) / 64) * ((n + 63) / 64) * 4u <= k / 64u);
+    const uint64_t tiles = ((m + 63) / 64) * ((n + 63) / 64);
+    return m <= 64 ? tiles < (m <= 32 ? 384u : 128u) : m <= 1024 && tiles <= 64;
 }
 
 template <typename T>
@@ -326,10 +332,15 @@ int launch_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb,
     const uint32_t large = (uint32_t)tiles(256), rest = large % 256u, whole = rest <= 128u ? large - rest : large;
     /* Large results go past the caches, where the operands are read from, if their rows are whole lines: 8192 x 11008 x 1024 131 -> 124 us,
      * but 8192 x 5001 x 512 40 -> 56. */
-    out.past = large >= 96 && whole_lines(out.c, out.ldc * sizeof(T));
-    if (large >= 96)
+    out.past = m > 64 && large >= 96 && whole_lines(out.c, out.ldc * sizeof(T));
+    /* The largest tiles that still give work to most compute units (us by tiles of 256, halved where they are few, 128 and 64: 2048 x 4096 x 4096
+     * 48, 52, 84; 1024 x 4096 x 4096 30, 25, 41; 4096 x 768 x 768 11, 9.3, 10; 1024 x 1536 x 1536 15, 11.5, 10).  Where the weights are read once,
+     * from memory, the ring is twice as long (48 x 11008 x 4096 20.4 -> 18.3). */
+    if (m <= 64)
+        k_product<T, 64, 8><<<(uint32_t)tiles(64), 256, 0, st>>>(a, lda, b, ldb, m, n, k, out);
+    else if (large >= 96)
         k_product_large<T><<<whole + (large - whole) * 2u, 512, 0, st>>>(a, lda, b, ldb, m, n, k, out, whole);
-    else if (tiles(128) >= 256)
+    else if (tiles(128) >= 160)
         k_product<T, 128, 4><<<(uint32_t)tiles(128), 256, 0, st>>>(a, lda, b, ldb, m, n, k, out);
     else
         k_product<T, 64, 4><<<(uint32_t)tiles(64), 256, 0, st>>>(a, lda, b, ldb, m, n, k, out);
@@ -345,10 +356,10 @@ extern "C" int nsml_q8_matmul(const int8_t *a, uint64_t lda, const float *a_scal
     if (n == 0 || k == 0 || bad_type(type) || bad_codes(b, ldb, k) || (b_scale && bad_f32(b_scale)) || (bias && bad_f32(bias)) ||
         (m && (bad_codes(a, lda, k) || bad_f32(a_scale) || bad_mat(c, type, ldc, n))))
         return NSML_EINVAL;
-    if (k > NSML_Q8_MAX_COLS || lda > MAX_LD || ldb > MAX_LD) return NSML_ECAP;
+    if (k > NSML_Q8_MAX_COLS || n > MAX_COLS || (m && lda > MAX_LD) || ldb > MAX_LD) return NSML_ECAP;
     if (m == 0) return NSML_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (by_few(m, n, k)) return launch_few(a, lda, b, ldb, m, n, k, AnyOut{c, ldc, a_scale, b_scale, bias, type}, st);
+    if (by_few(m, n)) return launch_few(a, lda, b, ldb, m, n, k, AnyOut{c, ldc, a_scale, b_scale, bias, type}, st);
     if (type == NSML_F32) return launch_product(a, lda, b, ldb, m, n, k, Out<float>{static_cast<float *>(c), ldc, a_scale, b_scale, bias, false}, st);
     if (type == NSML_BF16) return launch_product(a, lda, b, ldb, m, n, k, Out<bf16>{static_cast<bf16 *>(c), ldc, a_scale, b_scale, bias, false}, st);
     return launch_product(a, lda, b, ldb, m, n, k, Out<f16>{static_cast<f16 *>(c), ldc, a_scale, b_scale, bias, false}, st);

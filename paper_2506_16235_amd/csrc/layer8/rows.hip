@@ -490,6 +490,7 @@ int nsml_q8_values(const int8_t *q, uint64_t ldq, const float *scale, uint64_t r
 {
     if (cols == 0 || bad_type(type) || (rows && (bad_codes(q, ldq, cols) || (scale && bad_f32(scale)) || bad_mat(out, type, ldo, cols))))
         return NSML_EINVAL;
+    if (cols > MAX_COLS) return NSML_ECAP;
     return by_type(type, [&](auto v) {
         using T = decltype(v);
         return launch_each(OpValues<T>{mat<int8_t>((const void *)q, ldq), scale, mat<T>(out, ldo)}, rows, cols, (hipStream_t)stream);
@@ -499,6 +500,7 @@ int nsml_q8_values(const int8_t *q, uint64_t ldq, const float *scale, uint64_t r
 int nsml_ckpt8_pack(const void *x, int type, uint64_t ldx, uint64_t rows, uint32_t cols, const nsml_ckpt8 *out, void *stream)
 {
     if (cols == 0 || bad_type(type) || (rows && (bad_mat(x, type, ldx, cols) || bad_ckpt(out, cols)))) return NSML_EINVAL;
+    if (cols > MAX_COLS) return NSML_ECAP;
     return by_type(type, [&](auto v) {
         using T = decltype(v);
         return launch_each(OpPack<T>{mat<T>(x, ldx), ckpt_of(out)}, rows, cols, (hipStream_t)stream);
@@ -508,6 +510,7 @@ int nsml_ckpt8_pack(const void *x, int type, uint64_t ldx, uint64_t rows, uint32
 int nsml_ckpt8_unpack(const nsml_ckpt8 *x, uint64_t rows, uint32_t cols, void *out, int type, uint64_t ldo, void *stream)
 {
     if (cols == 0 || bad_type(type) || (rows && (bad_ckpt(x, cols) || bad_mat(out, type, ldo, cols)))) return NSML_EINVAL;
+    if (cols > MAX_COLS) return NSML_ECAP;
     return by_type(type, [&](auto v) {
         using T = decltype(v);
         return launch_each(OpUnpack<T>{ckpt_of(x), mat<T>(out, ldo)}, rows, cols, (hipStream_t)stream);
@@ -591,6 +594,7 @@ int nsml_swiglu_backward(const void *da, uint64_t ldda, const nsml_ckpt8 *gate, 
         (rows && (bad_mat(da, type, ldda, cols) || bad_ckpt(gate, cols) || bad_ckpt(up, cols) ||
                   bad_mat(dgate, type, lddg, cols) || bad_mat(dup, type, lddu, cols))))
         return NSML_EINVAL;
+    if (cols > MAX_COLS) return NSML_ECAP;
     return by_type(type, [&](auto v) {
         using T = decltype(v);
         return launch_each(OpGluBack<T>{mat<T>(da, ldda), ckpt_of(gate), ckpt_of(up), mat<T>(dgate, lddg), mat<T>(dup, lddu)}, rows, cols,

@@ -284,16 +284,18 @@ __global__ void __launch_bounds__(256) k_wgrad_sum(const float *part, const floa
     }
 }
 
-/* Side of the tiles and number of slices.  Tiles of 256 for bfloat16 where they fill the chip; the parts of the other types take
- * the room that they would need.  Where there are fewer tiles than the chip has room for (two workgroups a compute unit, one with
+/* Side of the tiles and number of slices.  Tiles of 256 for bfloat16 where those of 128 would be more than the chip has room for at a time
+ * (4096 rows, us by tiles of 256 and 128: 4096 x 4096 150, 205; 3328 x 3328 119, 163; 2048 x 4096 96, 97; 2048 x 2048 62, 61); the parts of the
+ * other types take the room that they would need.  Where there are fewer tiles than the chip has room for (two workgroups a compute unit, one with
  * parts), the rows are cut into slices: a stage of 64 rows less takes 1.2 us less, a slice more writes and reads 8 bytes more for each
- * element of dw, at about 4 TB/s, and what is least is taken (1027 x 768 x 768, us for 1, 4 and 8 slices: see the case table). */
+ * element of dw, at about 4 TB/s, and what is least is taken (1027 x 768 x 768 float16: 9 slices 33 us, 5 as taken 22; 300 x 2000 x 2000
+ * bfloat16: 2 slices 32, 1 as taken 15). */
 struct Shape { uint32_t side, slices; uint64_t tiles; };
 Shape shape_of(uint64_t rows, uint32_t n, uint32_t k, int type)
 {
     const auto tiles = [&](uint64_t s) { return ((n + s - 1) / s) * ((k + s - 1) / s); };
     const bool one = type == NSML_BF16;
-    const uint32_t side = one && tiles(256) >= 192 ? 256 : 128;
+    const uint32_t side = one && tiles(256) > 128 ? 256 : 128;
     const uint64_t stages = (rows + 63) / 64, room = (one && side == 128 ? 512 : 256) / tiles(side);
     const double stage_us = one ? 1.2 : type == NSML_F16 ? 1.9 : 2.5, slice_us = (double)n * k * 2e-6;
     uint64_t s = (uint64_t)std::sqrt(stage_us * (double)stages / slice_us);
@@ -342,6 +344,7 @@ int nsml_ckpt8_wgrad(const void *dy, int type, uint64_t lddy, const nsml_ckpt8 *
         return NSML_EINVAL;
     const uint64_t need = nsml_ckpt8_wgrad_work(rows, n, k);
     if (need && (!work || !at_multiple(work, 16) || work_bytes < need)) return NSML_EINVAL;
+    if (n > MAX_COLS || k > MAX_COLS) return NSML_ECAP;
     const Shape s = shape_of(rows, n, k, type);
     if (s.tiles >= (1u << 24) || (rows && (lddy >= MAX_LD || x->ldq >= MAX_LD || x->lde >= MAX_LD))) return NSML_ECAP;
     hipStream_t st = static_cast<hipStream_t>(stream);

@@ -31,6 +31,7 @@ def test_rows_and_values():
         return L.nsml_q8_values(q, ldq, s, m, k, out, type, ldo, None)
     for bad in ({"q": None}, {"ldq": 65}, {"s": P + 1}, {"k": 0}, {"out": None}, {"out": P + 1}, {"type": 9}, {"ldo": 10}):
         refused(values(**bad))
+    refused(values(k=(1 << 32) - 1, ldq=1 << 32, ldo=1 << 32), nsml.ECAP)
 
 
 def test_matmul():
@@ -41,6 +42,7 @@ def test_matmul():
         refused(mm(**bad))
     refused(mm(k=131088, lda=131088, ldb=131088), nsml.ECAP)
     refused(mm(lda=(1 << 22) + 16), nsml.ECAP)
+    refused(mm(n=(1 << 32) - 1, ldc=1 << 33), nsml.ECAP)
 
 
 def test_checkpoints():
@@ -65,6 +67,8 @@ def test_wgrad():
     for bad in ({"dy": None}, {"dy": P + 1}, {"type": 4}, {"lddy": 999}, {"col": P + 2}, {"n": 0}, {"k": 0}, {"add": P + 1}, {"dw": None},
                 {"ld": 63}, {"work": None}, {"work": P + 8}, {"size": L.nsml_ckpt8_wgrad_work(4000, 1000, 64) - 1}):
         refused(wg(**bad))
+    refused(wg(n=1 << 31, lddy=1 << 31), nsml.ECAP)
+    refused(wg(lddy=1 << 23), nsml.ECAP)
     assert L.nsml_ckpt8_wgrad_work(4000, 1000, 64) > 0 and L.nsml_ckpt8_wgrad_work(0, 1000, 64) == 0
 
 
