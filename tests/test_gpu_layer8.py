@@ -548,3 +548,61 @@ def test_on_another_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(held, step()))
+
+
+# ---------------------------------------------------------------- both sides of the sizes at which another launch is chosen
+
+@pytest.mark.parametrize("m,n,k", [(10, 6000, 70), (10, 20000, 300), (16, 24500, 48), (16, 24600, 48), (20, 6000, 520), (20, 9000, 257), (32, 20000, 1030),
+                                   (33, 8100, 300), (40, 6000, 515), (48, 8200, 100), (60, 6000, 999), (64, 8128, 40), (64, 8130, 1100),
+                                   (65, 4096, 100), (70, 2000, 333), (1000, 300, 64), (1030, 200, 64), (1000, 2600, 200), (1000, 2400, 81),
+                                   (3000, 3600, 140), (2500, 2500, 65), (2300, 2500, 127), (5100, 1290, 190)])
+def test_product_at_every_launch(m, n, k):
+    product_case(m, n, k, TYPES[(m + n + k) % 3], 3, with_b=n % 3 != 0, with_bias=k % 2 == 0)
+
+
+@types
+@pytest.mark.parametrize("m,n,k", [(2560, 2560, 192), (2500, 4096, 130), (4096, 4096, 77)])
+def test_product_whole_lines(dt, m, n, k):
+    """Large results whose rows are whole lines take another kind of store."""
+    g = gen(m + k)
+    a, b = torch.randint(-127, 128, (m, k), generator=g, dtype=torch.int8), torch.randint(-127, 128, (n, k), generator=g, dtype=torch.int8)
+    sa, sb = torch.rand(m, generator=g) + 0.1, torch.rand(n, generator=g) * 0.01 + 1e-3
+    c = nsml.q8_matmul(nsml.Q8(padded_codes(a), sa.to(DEV)), nsml.Q8(padded_codes(b), sb.to(DEV)), dt)
+    ref = (a.to(DEV).double() @ b.to(DEV).double().t().contiguous()) * sa.to(DEV).double()[:, None] * sb.to(DEV).double()
+    lim = (HALF[dt] + 4 * u32) * ref.abs() + (2.0 ** -25 if dt == torch.float16 else 0)
+    assert bool(((c.double() - ref).abs() <= lim).all())
+
+
+@pytest.mark.parametrize("m,n,k,col,add", [(70, 2944, 3328, True, None), (200, 3001, 3300, False, "apart"), (64, 3100, 2950, True, "self"),
+                                           (130, 2048, 4096, True, "apart"), (130, 2304, 4096, False, None), (1, 3000, 3001, True, None)])
+def test_wgrad_large_tiles(m, n, k, col, add):
+    wgrad_case(m, n, k, torch.bfloat16, col=col, add=add, seed=6)
+
+
+def test_wgrad_whole_lines_and_a_second_call():
+    m, n, k = 320, 3200, 3200
+    dy, x = (torch.randn(m, n, generator=gen(1)) * 1e-3).bfloat16().to(DEV), acts(2, m, k).to(DEV)
+    c = nsml.ckpt8_pack(x)
+    dw = nsml.ckpt8_wgrad(dy, c)
+    v = nsml.ckpt8_unpack(c).double()
+    ref, size = dy.double().t().contiguous() @ v, dy.double().abs().t().contiguous() @ v.abs()
+    assert bool(((dw.double() - ref).abs() <= 4 * u32 * ref.abs() + (4 + 2 * m ** 0.5) * u32 * size).all())
+    both = nsml.ckpt8_wgrad(dy, c, add=dw, out=dw)
+    assert both is dw and bool(((dw.double() - 2 * ref).abs() <= 8 * u32 * ref.abs() + (8 + 4 * m ** 0.5) * u32 * size).all())
+
+
+def test_rows_beyond_32_bits_of_bytes():
+    """Offsets of a long matrix pass 2^32."""
+    m, k = (1 << 32) // 4096 + 70, 4096
+    x = torch.zeros(m, k, dtype=torch.bfloat16, device=DEV)
+    tail = acts(1, 100, k, torch.bfloat16).to(DEV)
+    x[-100:] = tail
+    c, q = nsml.ckpt8_pack(x), nsml.q8_rows(x)
+    ct, qt = nsml.ckpt8_pack(tail), nsml.q8_rows(tail)
+    assert torch.equal(c.q[-100:], ct.q) and torch.equal(c.e[-100:], ct.e) and torch.equal(q.q[-100:], qt.q) and torch.equal(q.scale[-100:], qt.scale)
+    w = nsml.q8_rows(acts(2, 40, k).to(DEV))
+    assert torch.equal(nsml.q8_matmul(q, w)[-100:], nsml.q8_matmul(qt, w))
+    dy = torch.zeros(m, 8, dtype=torch.bfloat16, device=DEV)
+    dy[-100:] = torch.randn(100, 8, generator=gen(3)).to(torch.bfloat16).to(DEV)
+    a, b = nsml.ckpt8_wgrad(dy, c), nsml.ckpt8_wgrad(dy[-100:], ct)
+    assert bool(((a - b).abs() <= 64 * u32 * (dy[-100:].float().abs().t().contiguous() @ nsml.ckpt8_unpack(ct).abs())).all())
