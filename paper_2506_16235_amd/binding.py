@@ -503,46 +503,55 @@ _TYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _F32_ONLY, _I8_ONLY, _U8_ONLY = torch.float32, torch.int8, torch.uint8
 
 
-def _matrix(name, t, dev, dtype=None, rows=None, cols=None):
+def _matrix(name, t, dev, dtype=None, rows=None, cols=None, _Tensor=torch.Tensor):
     """-> (address, elements from row to row, rows, cols) of a matrix whose rows are contiguous."""
+    if isinstance(t, _Tensor):
+        shape = t.shape
+        if len(shape) == 2:
+            r, c = shape
+            ld, side = t.stride()
+            if ((t.dtype in _TYPE if dtype is None else t.dtype is dtype) and t.device == dev and c
+                    and (rows is None or r == rows) and (cols is None or c == cols)
+                    and (side == 1 or c == 1 or not r) and (ld >= c or r <= 1)):
+                return t.data_ptr(), (ld if ld > c else c), r, c
+    raise ValueError(_why_not(name, t, dev, dtype, rows, cols))
+
+
+def _why_not(name, t, dev, dtype, rows, cols) -> str:
+    """What _matrix refuses a matrix for."""
     if not isinstance(t, torch.Tensor):
-        raise ValueError(f"{name} must be a torch tensor")
+        return f"{name} must be a torch tensor"
     if t.dim() != 2:
-        raise ValueError(f"{name} has {t.dim()} dimensions, needs 2")
+        return f"{name} has {t.dim()} dimensions, needs 2"
     if t.device != dev:
-        raise ValueError(f"{name} is on {t.device}, not on {dev}")
+        return f"{name} is on {t.device}, not on {dev}"
     if (t.dtype not in _TYPE) if dtype is None else (t.dtype != dtype):
-        raise ValueError(f"{name} has dtype {t.dtype}")
+        return f"{name} has dtype {t.dtype}"
     r, c = t.shape
     if (rows is not None and r != rows) or (cols is not None and c != cols):
-        raise ValueError(f"{name} is {r} x {c}, needs {r if rows is None else rows} x {c if cols is None else cols}")
+        return f"{name} is {r} x {c}, needs {r if rows is None else rows} x {c if cols is None else cols}"
     if c == 0:
-        raise ValueError(f"{name} has no columns")
-    ld, side = t.stride()
-    if (side != 1 and c > 1 and r) or (ld < c and r > 1):
-        raise ValueError(f"{name} has strides {t.stride()}: rows must be contiguous and must not overlap")
-    return t.data_ptr(), max(ld, c), r, c
+        return f"{name} has no columns"
+    return f"{name} has strides {t.stride()}: rows must be contiguous and must not overlap"
 
 
-def _vector(name, t, dev, n):
+def _vector(name, t, dev, n, _Tensor=torch.Tensor):
     """-> address of a float32 vector, or None."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or t.device != dev or t.dtype != _F32_ONLY or t.dim() != 1 or t.shape[0] != n \
-            or (n > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name} must be a contiguous float32 vector of {n} elements on {dev}")
-    return t.data_ptr()
+    if isinstance(t, _Tensor) and t.dtype is _F32_ONLY and t.shape == (n,) and t.device == dev and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name} must be a contiguous float32 vector of {n} elements on {dev}")
 
 
 def _codes(name, t, dev, rows=None, cols=None):
     """_matrix of int8 codes: 16-byte aligned rows that own their bytes up to the next multiple of 16."""
     at, ld, r, c = _matrix(name, t, dev, _I8_ONLY, rows, cols)
-    room = (c + 15) // 16 * 16
     if r <= 1:
-        ld = room
-    if ld % 16 or at % 16:
+        ld = (c + 15) & ~15
+    if (ld | at) & 15:
         raise ValueError(f"{name}: rows of codes must start at multiples of 16 bytes (strides {t.stride()})")
-    if room != c and r and t.storage_offset() + (r - 1) * ld + room > t.untyped_storage().nbytes():
+    if c & 15 and r and t.storage_offset() + (r - 1) * ld + ((c + 15) & ~15) > t.untyped_storage().nbytes():
         raise ValueError(f"{name}: the last row of codes must own its bytes up to the next multiple of 16")
     return at, ld, r, c
 
