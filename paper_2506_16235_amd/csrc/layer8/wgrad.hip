@@ -295,7 +295,8 @@ Shape shape_of(uint64_t rows, uint32_t n, uint32_t k, int type)
 {
     const auto tiles = [&](uint64_t s) { return ((n + s - 1) / s) * ((k + s - 1) / s); };
     const bool one = type == NSML_BF16;
-    const uint32_t side = one && tiles(256) > 128 ? 256 : 128;
+    /* (a matrix that a side of 128 holds gains nothing from a larger one, and those of fewer than four columns have tiles of 128 only) */
+    const uint32_t side = one && n > 128 && k > 128 && tiles(256) > 128 ? 256 : 128;
     const uint64_t stages = (rows + 63) / 64, room = (one && side == 128 ? 512 : 256) / tiles(side);
     const double stage_us = one ? 1.2 : type == NSML_F16 ? 1.9 : 2.5, slice_us = (double)n * k * 2e-6;
     uint64_t s = (uint64_t)std::sqrt(stage_us * (double)stages / slice_us);

@@ -606,3 +606,10 @@ def test_rows_beyond_32_bits_of_bytes():
     dy[-100:] = torch.randn(100, 8, generator=gen(3)).to(torch.bfloat16).to(DEV)
     a, b = nsml.ckpt8_wgrad(dy, c), nsml.ckpt8_wgrad(dy[-100:], ct)
     assert bool(((a - b).abs() <= 64 * u32 * (dy[-100:].float().abs().t().contiguous() @ nsml.ckpt8_unpack(ct).abs())).all())
+
+
+@types
+@pytest.mark.parametrize("m,n,k", [(33, 3, 33000), (40, 1, 65700), (64, 100, 34000), (20, 34000, 3), (70, 33100, 60)])
+def test_wgrad_long_and_narrow(dt, m, n, k):
+    """Many tiles of a matrix with few rows or columns."""
+    wgrad_case(m, n, k, dt, col=n < k, add=None, seed=7)
