@@ -18,10 +18,7 @@ template <typename T> struct Out {
 
 /* ---------------------------------------------------------------- tiles */
 
-/* A stage of a tile in LDS: 64 bytes of k of each row, four rows to 256 bytes (all the banks once), whose sixteen chunks of 16 bytes
- * lie there in an order that is another one for each of four neighbouring fours: the same chunk of 16 rows meets every bank once. */
-constexpr uint32_t DEPTH = 64;
-__device__ __forceinline__ uint32_t spot(uint32_t row, uint32_t chunk) { return row / 4u * 256u + (((row % 4u * 4u + chunk) ^ (row / 4u % 4u)) * 16u); }
+constexpr uint32_t DEPTH = 64;               /* bytes of k to a stage */
 
 /* A tile of BM x BN by WM x WN wavefronts.  Stages go from memory straight into a ring of places in LDS, all but one ahead; a wavefront's
  * requests are spread between its matrix instructions, as one that waits to make a request multiplies nothing.  The matrix instructions of

@@ -1,7 +1,7 @@
 /*
  * Tiles in LDS for the matrix instructions, shared by the products and the weight gradient.
  *
- * The products' rows (spot) are 64 bytes of the summed dimension, the weight gradient's (place) 128.  Measured here for accesses of 16
+ * The products' rows, and those of the weight gradient in parts, are 64 bytes of the summed dimension (spot), else 128 (place).  Measured here for accesses of 16
  * bytes per lane: a read takes 16 lanes a cycle (lanes 0-3, 12-15, 20-23 and 24-27, and so on) and a write eight neighbouring
  * ones, over 256 and 128 bytes of banks.  So the chunks of 16 bytes lie within 256 bytes in an order that differs from pair (place) or
  * four (spot) of rows to the next, such that reads of the same chunk of 32 rows, and writes of the same chunk of
@@ -30,7 +30,10 @@ __device__ __forceinline__ uint32_t place(uint32_t row, uint32_t chunk)
 {
     return row / 2u * 256u + ((row % 2u * 12u ^ chunk ^ row / 2u % 8u) * 16u);
 }
-constexpr uint32_t BLOCK = 32 * 128;                 /* bytes from one block of 32 rows to the next */
+__device__ __forceinline__ uint32_t spot(uint32_t row, uint32_t chunk)
+{
+    return row / 4u * 256u + (((row % 4u * 4u + chunk) ^ (row / 4u % 4u)) * 16u);
+}
 
 /* What a lane gives a matrix instruction of 32 x 32: 16 bytes of one row of a block. */
 __device__ __forceinline__ v4i frag(const uint8_t *at) { return *reinterpret_cast<const v4i *>(at); }

@@ -38,26 +38,33 @@ template <typename T> struct Wgrad {
     bool past;                   /* dw past the caches */
 };
 
-/* A tile of BN x BK of dw by WM x WN wavefronts, one slice of the rows, 64 rows to a stage.  Every thread brings eight rows of four
- * neighbours of both operands: the next stage's wait in registers while this one is multiplied and go to the other half of
- * LDS between its matrix instructions, which leave the vector unit three quarters of its time.  Neighbour j of the four goes to row
- * j * BN / 4 + group of LDS: writes meet no bank twice, and a wavefront whose blocks are the four neighbours of 32 groups holds four
- * neighbours of dw in a lane.  NARROW: n < 4. */
+/* Rows of a stage.  With parts half as many: two stages of a tile of 256 then fit LDS, and two workgroups with tiles of 128 a compute unit
+ * (us with 64 rows, for which only tiles of 128 fit, and with 32: 8192 x 4096 x 4096 float16 743, 447, binary32 939, 619; 4096 x 2048 x 4096
+ * by tiles of 128 both 188, 156 and 235, 208). */
+template <typename T> constexpr int ROWS = PARTS<T> == 1 ? 64 : 32;
+/* Where chunk c (eight rows of the stage) of a row of LDS lies. */
+template <int N> __device__ __forceinline__ uint32_t spot_of(uint32_t row, uint32_t c) { return N == 64 ? place(row, c) : spot(row, c); }
+
+/* A tile of BN x BK of dw by WM x WN wavefronts, one slice of the rows, ROWS to a stage.  Every thread brings an eighth of a stage's rows of
+ * four neighbours of both operands: the next stage's wait in registers while this one is multiplied and go to the other half of LDS
+ * between its matrix instructions, which leave the vector unit three quarters of its time.  Neighbour j of the four goes to row
+ * j * BN / 4 + group of LDS: a wavefront whose blocks are the four neighbours of 32 groups holds four neighbours of dw in a lane.
+ * NARROW: n < 4. */
 template <typename T, int BN, int BK, int WM, int WN, bool NARROW>
 __global__ void __launch_bounds__(WM * WN * 64)
 k_wgrad(Wgrad<T> g)
 {
-    constexpr int P = PARTS<T>, W = WM * WN, TM = BN / WM / 32, TN = 4, WD = WORDS<T>;
-    constexpr int STAGE = (P * BN + BK) * 128;
-    static_assert(BN == W * 32 && BK == BN && BK == WN * 128, "a unit of 8 x 4 of both operands per thread, 128 columns per wavefront");
+    constexpr int P = PARTS<T>, N = ROWS<T>, R = N / 8, LINE = N * 2, W = WM * WN, TM = BN / WM / 32, TN = 4, WD = WORDS<T>;
+    constexpr int STAGE = (P * BN + BK) * LINE;
+    static_assert(BN == W * 32 && BK == BN && BK == WN * 128, "a unit of an eighth x 4 of both operands per thread, 128 columns per wavefront");
     __shared__ __align__(16) uint8_t lds[2 * STAGE];
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const Tile tile = tile_of(blockIdx.x, (g.n + BN - 1) / BN, (g.k + BK - 1) / BK);
     const uint32_t n0 = tile.row * BN, k0 = tile.col * BK;
-    const uint64_t stages = (g.rows + 63) / 64;
+    const uint64_t stages = (g.rows + N - 1) / N;
     const uint64_t from = stages * blockIdx.y / g.slices, to = stages * (blockIdx.y + 1) / g.slices;
     const uint32_t wm = wave / WN * (BN / WM), wn = wave % WN * 32u;        /* rows of LDS */
-    const uint32_t group = threadIdx.x % (BN / 4), chunk = threadIdx.x / (BN / 4);
+    const uint32_t group = threadIdx.x % (BN / 4), part = threadIdx.x / (BN / 4);
     /* Columns beyond the matrices: any that are there, as what comes of them is not stored.  The four that a row of dy ends in are read
      * from the last four, and moved (n >= 4), or one by one. */
     const uint32_t cd = n0 + group * 4u, cx = k0 + group * 4u;
@@ -65,18 +72,18 @@ k_wgrad(Wgrad<T> g)
     const uint32_t at_d = (cd + 4u <= g.n ? cd : NARROW ? 0u : g.n - 4u) * (uint32_t)sizeof(T);
     const uint32_t at_x = cx < g.k ? cx : 0u, at_e = at_x / 32u;
     const uint32_t ld_d = (uint32_t)g.dy.ld * (uint32_t)sizeof(T), ld_x = (uint32_t)g.x.ldq, ld_e = (uint32_t)g.x.lde;
-    uint32_t d[8][WD], q[8], e[8];
+    uint32_t d[R][WD], q[R], e[R];
 
     /* Where a thread's first row lies; the others are whole rows away, which is the same for all threads. */
-    const uint32_t to_d = __umul24(chunk * 8u, ld_d) + at_d, to_x = __umul24(chunk * 8u, ld_x) + at_x, to_e = __umul24(chunk * 8u, ld_e) + at_e;
+    const uint32_t to_d = __umul24(part * R, ld_d) + at_d, to_x = __umul24(part * R, ld_x) + at_x, to_e = __umul24(part * R, ld_e) + at_e;
     auto fetch = [&](uint64_t stage, auto edge) {
-        const uint64_t row0 = stage * 64u;
+        const uint64_t row0 = stage * N;
         const uint8_t *pd = reinterpret_cast<const uint8_t *>(g.dy.p) + row0 * ld_d;
         const uint8_t *px = reinterpret_cast<const uint8_t *>(g.x.q) + row0 * ld_x;
         const uint8_t *pe = g.x.e + row0 * ld_e;
-        const uint32_t last = (uint32_t)min<uint64_t>(g.rows - row0, 64u) - 1u;
+        const uint32_t last = (uint32_t)min<uint64_t>(g.rows - row0, N) - 1u;
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
+        for (int i = 0; i < R; i++) {
             Global rd = (Global)(pd + i * ld_d), rx = (Global)(px + i * ld_x), re = (Global)(pe + i * ld_e);
             if constexpr (!edge.value) {
                 uint32_t od = to_d, ox = to_x, oe = to_e;
@@ -84,7 +91,7 @@ k_wgrad(Wgrad<T> g)
                 asm("" : "+v"(od), "+v"(ox), "+v"(oe));      /* the load itself: no addition of 64 bits per load */
                 rd += od, rx += ox, re += oe;
             } else {                         /* rows beyond the matrix: its last one */
-                const uint32_t row = min(chunk * 8u + i, last);
+                const uint32_t row = min(part * R + i, last);
                 rd = (Global)pd + (__umul24(row, ld_d) + at_d), rx = (Global)px + (__umul24(row, ld_x) + at_x), re = (Global)pe + (__umul24(row, ld_e) + at_e);
             }
             q[i] = *(const __attribute__((address_space(1))) uint32_t *)rx;
@@ -103,11 +110,11 @@ k_wgrad(Wgrad<T> g)
     };
     /* What was read where a matrix ends: rows beyond it become zeros, the four that a row of dy ends in were read with those before. */
     auto mend = [&](uint64_t stage) {
-        const uint64_t have = g.rows - stage * 64u;
-        if (have < 64u) {
+        const uint64_t have = g.rows - stage * N;
+        if (have < N) {
 #pragma unroll
-            for (int i = 0; i < 8; i++)
-                if (chunk * 8u + i >= have) {
+            for (int i = 0; i < R; i++)
+                if (part * R + i >= have) {
                     q[i] = e[i] = 0;
 #pragma unroll
                     for (int w = 0; w < WD; w++) d[i][w] = 0;
@@ -116,7 +123,7 @@ k_wgrad(Wgrad<T> g)
         if (ends)
             for (uint32_t s = g.n % 4u; s < 4u; s++)
 #pragma unroll
-                for (int i = 0; i < 8; i++) {
+                for (int i = 0; i < R; i++) {
                     if constexpr (sizeof(T) == 2) {
                         d[i][0] = __builtin_amdgcn_alignbit(d[i][1], d[i][0], 16);
                         d[i][1] >>= 16;
@@ -125,11 +132,12 @@ k_wgrad(Wgrad<T> g)
                     }
                 }
     };
-    /* Neighbour j of the four, of both operands, as eight rows side by side. */
+    /* Neighbour j of the four, of both operands, as rows side by side: a chunk, or half of one. */
     auto put = [&](uint8_t *stage, int j) {
-        v4i p[P];
+        typedef int Out __attribute__((ext_vector_type(R / 2)));
+        Out p[P], x;
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
+        for (int i = 0; i < R / 2; i++) {
             if constexpr (P == 1) {
                 p[0][i] = (int)__builtin_amdgcn_perm(d[2 * i + 1][j / 2], d[2 * i][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
             } else {
@@ -145,51 +153,47 @@ k_wgrad(Wgrad<T> g)
                     v[0] = left_of(v[0]), v[1] = left_of(v[1]);
                 }
             }
-        }
-        const uint32_t at = place(j * (BN / 4) + group, chunk);
-#pragma unroll
-        for (int s = 0; s < P; s++) *reinterpret_cast<v4i *>(stage + s * BN * 128 + at) = p[s];
-        v4i x;
-#pragma unroll
-        for (int i = 0; i < 4; i++)
             x[i] = (int)upper2((float)(int8_t)(q[2 * i] >> (j * 8)) * ckpt_scale(e[2 * i]),
                                (float)(int8_t)(q[2 * i + 1] >> (j * 8)) * ckpt_scale(e[2 * i + 1]));
-        *reinterpret_cast<v4i *>(stage + P * BN * 128 + at) = x;
+        }
+        const uint32_t row = j * (BN / 4) + group, at = N == 64 ? spot_of<N>(row, part) : spot_of<N>(row, part / 2) + part % 2 * 8u;
+#pragma unroll
+        for (int s = 0; s < P; s++) *reinterpret_cast<Out *>(stage + s * BN * LINE + at) = p[s];
+        *reinterpret_cast<Out *>(stage + P * BN * LINE + at) = x;
     };
 
     v16f acc[TM][TN] = {};
-    const uint32_t ra = place(wm + lane % 32, lane / 32), rb = P * BN * 128 + place(wn + lane % 32, lane / 32);
-    v8bf fa[2][P][TM], fb[2][TN];
-    auto read = [&](uint32_t stage, int s) {
+    const uint32_t ra = spot_of<N>(wm + lane % 32, lane / 32), rb = P * BN * LINE + spot_of<N>(wn + lane % 32, lane / 32);
+    /* A stage is multiplied in U turns, 16 rows of one part of dy each, the smallest part first. */
+    constexpr int U = N / 16 * P, ALL = TM * TN;
+    static_assert(U % 2 == 0 && U >= 4, "two sets of registers by turns");
+    v8bf fa[2][TM], fb[2][TN];
+    auto read = [&](uint32_t stage, int u) {
+        const int s = u / P, p = P - 1 - u % P;
         const uint8_t *at_a = lds + ((ra + stage) ^ (s * 32u)), *at_b = lds + ((rb + stage) ^ (s * 32u));
+        if (u % P == 0)
 #pragma unroll
-        for (int j = 0; j < TN; j++) fb[s & 1][j] = __builtin_bit_cast(v8bf, frag(at_b + j * (BK / 4 * 128)));
+            for (int j = 0; j < TN; j++) fb[s & 1][j] = __builtin_bit_cast(v8bf, frag(at_b + j * (BK / 4 * LINE)));
 #pragma unroll
-        for (int p = 0; p < P; p++)
-#pragma unroll
-            for (int i = 0; i < TM; i++) fa[s & 1][p][i] = __builtin_bit_cast(v8bf, frag(at_a + p * BN * 128 + i * BLOCK));
+        for (int i = 0; i < TM; i++) fa[u & 1][i] = __builtin_bit_cast(v8bf, frag(at_a + p * BN * LINE + i * 32 * LINE));
     };
-    /* The smallest parts first. */
-    auto multiply = [&](int s, int from, int to) {
+    auto multiply = [&](int u, int from, int to) {
 #pragma unroll
-        for (int t = from; t < to; t++) {
-            const int p = P - 1 - t / (TM * TN), i = t / TN % TM, j = t % TN;
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[s & 1][p][i], fb[s & 1][j], acc[i][j], 0, 0, 0);
-        }
+        for (int t = from; t < to; t++)
+            acc[t / TN][t % TN] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[u & 1][t / TN], fb[u / P & 1][t % TN], acc[t / TN][t % TN], 0, 0, 0);
     };
-    constexpr int ALL = P * TM * TN;
-    /* One quarter of a stage: its first product waits for what it multiplies, the next quarter is read behind the others, with
+    /* One turn: its first product waits for what it multiplies, the next turn's is read behind the others, with
      * `work` for the vector unit between them. */
-    auto quarter = [&](uint32_t next, int s, auto work) {
+    auto turn = [&](uint32_t next, int u, auto work) {
         wait_lds();
-        multiply(s, 0, 1);
+        multiply(u, 0, 1);
         __builtin_amdgcn_sched_barrier(0);
-        read(next, (s + 1) % 4);
+        read(next, (u + 1) % U);
         __builtin_amdgcn_sched_barrier(0);
-        multiply(s, 1, ALL);
+        multiply(u, 1, ALL);
         work();
     };
-    /* What the vector unit does in a quarter goes between its products, some instructions behind each. */
+    /* What the vector unit does in a turn goes between its products, some instructions behind each. */
     auto between = [&]() {
 #pragma unroll
         for (int t = 1; t < ALL; t++) {
@@ -198,6 +202,8 @@ k_wgrad(Wgrad<T> g)
         }
         __builtin_amdgcn_sched_barrier(0);
     };
+    /* The turn in which neighbour j is put: the last ones before the barrier, as what was asked for has then had the longest time to come. */
+    constexpr auto turn_of = [](int j) { return U == 4 ? (j ? 2 : 1) : U - 5 + j; };
     /* edge: the tile or the slice holds an end of the matrices. */
     auto all = [&](auto edge) {
         fetch(from, edge);
@@ -210,21 +216,26 @@ k_wgrad(Wgrad<T> g)
         read(0, 0);
         uint32_t at = 0;
         for (uint64_t stage = from; stage < to; stage++, at ^= STAGE) {
-            quarter(at, 0, [] {});
-            __builtin_amdgcn_sched_barrier(0);
-            if constexpr (edge.value) mend(min(stage + 1, to - 1));
-            quarter(at, 1, [&] { put(lds + (at ^ STAGE), 0); });
-            between();
-            quarter(at, 2, [&] { put(lds + (at ^ STAGE), 1); put(lds + (at ^ STAGE), 2); put(lds + (at ^ STAGE), 3); });
-            between();
+#pragma unroll
+            for (int u = 0; u < U - 1; u++) {
+                if constexpr (edge.value)
+                    if (u == turn_of(0)) mend(min(stage + 1, to - 1));
+                turn(at, u, [&] {
+#pragma unroll
+                    for (int j = 0; j < 4; j++)
+                        if (turn_of(j) == u) put(lds + (at ^ STAGE), j);
+                });
+                if (u >= turn_of(0)) between();
+                else __builtin_amdgcn_sched_barrier(0);
+            }
             wg_sync();                       /* the next stage is there, and this one is in registers everywhere */
             fetch(min(stage + 2, to - 1), edge);         /* (between the products: the same within 2 %) */
             __builtin_amdgcn_sched_barrier(0);
-            quarter(at ^ STAGE, 3, [] {});
+            turn(at ^ STAGE, U - 1, [] {});
         }
     };
     if (from < to) {
-        if (NARROW || n0 + BN > g.n || to * 64u > g.rows) all(std::true_type{});
+        if (NARROW || n0 + BN > g.n || to * N > g.rows) all(std::true_type{});
         else all(std::false_type{});
     }
     const uint32_t c = k0 + (wn + lane % 32) * 4u;
@@ -284,20 +295,19 @@ __global__ void __launch_bounds__(256) k_wgrad_sum(const float *part, const floa
     }
 }
 
-/* Side of the tiles and number of slices.  Tiles of 256 for bfloat16 where those of 128 would be more than the chip has room for at a time
- * (4096 rows, us by tiles of 256 and 128: 4096 x 4096 150, 205; 3328 x 3328 119, 163; 2048 x 4096 96, 97; 2048 x 2048 62, 61); the parts of the
- * other types take the room that they would need.  Where there are fewer tiles than the chip has room for (two workgroups a compute unit, one with
- * parts), the rows are cut into slices: a stage of 64 rows less takes 1.2 us less, a slice more writes and reads 8 bytes more for each
- * element of dw, at about 4 TB/s, and what is least is taken (1027 x 768 x 768 float16: 9 slices 33 us, 5 as taken 22; 300 x 2000 x 2000
- * bfloat16: 2 slices 32, 1 as taken 15). */
+/* Side of the tiles and number of slices.  Tiles of 256 where those of 128 would be more than the chip has room for at a time (4096 rows of
+ * bfloat16, us by tiles of 256 and 128: 4096 x 4096 150, 205; 3328 x 3328 119, 163; 2048 x 4096 96, 97; 2048 x 2048 62, 61).  Where there are
+ * fewer tiles than the chip has room for (two workgroups a compute unit), the rows are cut into slices: 64 rows less take 1.2 us less (1.9
+ * and 2.5 with two and three parts), a slice more writes and reads 8 bytes more for each element of dw, at about 4 TB/s, and what is least is
+ * taken (1027 x 768 x 768 float16: 9 slices 33 us, 5 as taken 21; 300 x 2000 x 2000 bfloat16: 2 slices 32, 1 as taken 15). */
 struct Shape { uint32_t side, slices; uint64_t tiles; };
 Shape shape_of(uint64_t rows, uint32_t n, uint32_t k, int type)
 {
     const auto tiles = [&](uint64_t s) { return ((n + s - 1) / s) * ((k + s - 1) / s); };
     const bool one = type == NSML_BF16;
     /* (a matrix that a side of 128 holds gains nothing from a larger one, and those of fewer than four columns have tiles of 128 only) */
-    const uint32_t side = one && n > 128 && k > 128 && tiles(256) > 128 ? 256 : 128;
-    const uint64_t stages = (rows + 63) / 64, room = (one && side == 128 ? 512 : 256) / tiles(side);
+    const uint32_t side = n > 128 && k > 128 && tiles(256) > 128 ? 256 : 128;
+    const uint64_t stages = (rows + 63) / 64, room = (side == 128 ? 512 : 256) / tiles(side);
     const double stage_us = one ? 1.2 : type == NSML_F16 ? 1.9 : 2.5, slice_us = (double)n * k * 2e-6;
     uint64_t s = (uint64_t)std::sqrt(stage_us * (double)stages / slice_us);
     s = std::min(std::min(s, room), stages / 2);
@@ -307,13 +317,9 @@ Shape shape_of(uint64_t rows, uint32_t n, uint32_t k, int type)
 template <typename T> int launch_wgrad(const Wgrad<T> &g, const Shape &s, hipStream_t st)
 {
     const dim3 grid((uint32_t)s.tiles, s.slices);
-    if constexpr (PARTS<T> == 1) {
-        if (s.side == 256) k_wgrad<T, 256, 256, 4, 2, false><<<grid, 512, 0, st>>>(g);
-    }
-    if (s.side == 128) {
-        if (g.n < 4) k_wgrad<T, 128, 128, 4, 1, true><<<grid, 256, 0, st>>>(g);
-        else k_wgrad<T, 128, 128, 4, 1, false><<<grid, 256, 0, st>>>(g);
-    }
+    if (s.side == 256) k_wgrad<T, 256, 256, 4, 2, false><<<grid, 512, 0, st>>>(g);
+    else if (g.n < 4) k_wgrad<T, 128, 128, 4, 1, true><<<grid, 256, 0, st>>>(g);
+    else k_wgrad<T, 128, 128, 4, 1, false><<<grid, 256, 0, st>>>(g);
     const int rc = launched();
     if (rc || s.slices == 1) return rc;
     uint32_t log2l = 0;

@@ -613,3 +613,9 @@ def test_rows_beyond_32_bits_of_bytes():
 def test_wgrad_long_and_narrow(dt, m, n, k):
     """Many tiles of a matrix with few rows or columns."""
     wgrad_case(m, n, k, dt, col=n < k, add=None, seed=7)
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.float32], ids=["f16", "f32"])
+@pytest.mark.parametrize("m,n,k,col,add", [(70, 2944, 3328, True, None), (201, 3001, 3300, False, "apart"), (32, 3100, 2950, True, "self"), (1, 3000, 3001, True, None)])
+def test_wgrad_large_tiles_in_parts(dt, m, n, k, col, add):
+    wgrad_case(m, n, k, dt, col=col, add=add, seed=8)
