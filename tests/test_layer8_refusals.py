@@ -168,3 +168,9 @@ def test_binding_checks_vectors_and_pairs():
         nsml._ckpt("c", nsml.Ckpt8(q, torch.zeros(4, 1, dtype=torch.uint8)), CPU)       # needs two exponents a row
     with pytest.raises(ValueError):
         nsml._ckpt("c", nsml.Q8(q, torch.ones(4)), CPU)
+
+
+def test_results_of_more_tiles_than_a_launch_has():
+    for m, n in ((1, 1 << 30), (64, (1 << 30) - 32768 + 1), (1 << 31, 1), (1 << 29, 1024)):
+        refused(L.nsml_q8_matmul(P, 16, P, P, 16, P, None, m, n, 16, P, 1, n, None), nsml.ECAP)
+    refused(L.nsml_ckpt8_wgrad(P, 1, 1 << 21, ck(ldq=1 << 21, lde=1 << 16), None, 3, 1 << 21, 1 << 21, None, P, 1 << 21, P, 1 << 40, None), nsml.ECAP)
