@@ -295,23 +295,38 @@ __global__ void __launch_bounds__(256) k_wgrad_sum(const float *part, const floa
     }
 }
 
-/* Side of the tiles and number of slices.  Tiles of 256 where those of 128 would be more than the chip has room for at a time (4096 rows of
- * bfloat16, us by tiles of 256 and 128: 4096 x 4096 150, 205; 3328 x 3328 119, 163; 2048 x 4096 96, 97; 2048 x 2048 62, 61).  Where there are
- * fewer tiles than the chip has room for (two workgroups a compute unit), the rows are cut into slices: 64 rows less take 1.2 us less (1.9
- * and 2.5 with two and three parts), a slice more writes and reads 8 bytes more for each element of dw, at about 4 TB/s, and what is least is
- * taken (1027 x 768 x 768 float16: 9 slices 33 us, 5 as taken 21; 300 x 2000 x 2000 bfloat16: 2 slices 32, 1 as taken 15). */
+/* Side of the tiles and number of slices of the rows: what is least by the time that it should take, of what fills one, two or three rounds of
+ * 256 compute units, what balances the rows' time with that of joining the slices, and one slice.  Per 64 rows of a round, tiles of 256 take
+ * `large` us, tiles of 128 `alone` where a compute unit has one of them and `two` where it has two; a round takes 1.3 us to begin and end;
+ * joining takes 3 us, and for each slice 0.1 us and 8 bytes more for each element of dw (at 7 TB/s, part of them from caches).  Against the
+ * least of all sides and slices, measured for 60 sizes of three types, what is taken was 1 % slower in the mean and 15 % at most (us of the
+ * side / slices taken, and of others: bfloat16 8000 x 5000 x 1000 256/3 109, 128/1 201, 256/1 234; 8192 x 2048 x 2048 256/4 88, 256/3 96,
+ * 128/1 139; 600 x 1200 x 1200 128/1 18, 128/4 24; float16 1027 x 768 x 768 128/5 21, 128/1 32; 4000 x 300 x 11008 256/5 105, 128/1 150).  A
+ * side of 128 or less has tiles of 128, which hold it; those of fewer than four columns have no other kernel. */
 struct Shape { uint32_t side, slices; uint64_t tiles; };
+struct Rates { double large, alone, two; };
 Shape shape_of(uint64_t rows, uint32_t n, uint32_t k, int type)
 {
-    const auto tiles = [&](uint64_t s) { return ((n + s - 1) / s) * ((k + s - 1) / s); };
-    const bool one = type == NSML_BF16;
-    /* (a matrix that a side of 128 holds gains nothing from a larger one, and those of fewer than four columns have tiles of 128 only) */
-    const uint32_t side = n > 128 && k > 128 && tiles(256) > 128 ? 256 : 128;
-    const uint64_t stages = (rows + 63) / 64, room = (side == 128 ? 512 : 256) / tiles(side);
-    const double stage_us = one ? 1.2 : type == NSML_F16 ? 1.9 : 2.5, slice_us = (double)n * k * 2e-6;
-    uint64_t s = (uint64_t)std::sqrt(stage_us * (double)stages / slice_us);
-    s = std::min(std::min(s, room), stages / 2);
-    return {side, s < 2 ? 1u : (uint32_t)s, tiles(side)};
+    const Rates r = type == NSML_BF16 ? Rates{1.9, 0.95, 1.25} : type == NSML_F16 ? Rates{2.95, 1.45, 1.95} : Rates{3.8, 1.9, 2.5};
+    const uint64_t stages = (rows + 63) / 64;
+    const double slice = 0.1 + (double)n * k * 1.15e-6;
+    Shape best{};
+    double least = 0.0;
+    for (uint32_t side : {128u, 256u}) {
+        if (side == 256 && (n <= 128 || k <= 128)) continue;
+        const uint64_t tiles = ((uint64_t)n + side - 1) / side * (((uint64_t)k + side - 1) / side);
+        const uint64_t even = (uint64_t)std::sqrt((side == 256 ? r.large : r.alone) * (double)stages / slice);
+        for (uint64_t s : {uint64_t(1), 256 / tiles, 512 / tiles, 768 / tiles, std::min(even, 512 / tiles)}) {
+            if (s == 0 || (s > 1 && s > stages)) continue;
+            const uint64_t groups = tiles * s, per = (stages + s - 1) / s;
+            const uint64_t full = groups / (side == 256 ? 256 : 512), rest = groups % (side == 256 ? 256 : 512);
+            const double one = side == 256 ? r.large : r.two, last = side == 128 && rest <= 256 ? r.alone : one;
+            const double join = s > 1 ? 3.0 + (double)s * slice : 0.0;
+            const double us = (double)full * ((double)per * one + 1.3) + (rest ? (double)per * last + 1.3 : 0.0) + join;
+            if (best.side == 0 || us < least) best = {side, (uint32_t)s, tiles}, least = us;
+        }
+    }
+    return best;
 }
 
 template <typename T> int launch_wgrad(const Wgrad<T> &g, const Shape &s, hipStream_t st)

@@ -619,3 +619,10 @@ def test_wgrad_long_and_narrow(dt, m, n, k):
 @pytest.mark.parametrize("m,n,k,col,add", [(70, 2944, 3328, True, None), (201, 3001, 3300, False, "apart"), (32, 3100, 2950, True, "self"), (1, 3000, 3001, True, None)])
 def test_wgrad_large_tiles_in_parts(dt, m, n, k, col, add):
     wgrad_case(m, n, k, dt, col=col, add=add, seed=8)
+
+
+@types
+@pytest.mark.parametrize("m,n,k", [(3501, 3001, 900), (2100, 1300, 1100), (4001, 300, 1100), (700, 3000, 520), (3000, 129, 140), (3333, 1030, 260)])
+def test_wgrad_slices(dt, m, n, k):
+    """Slices of the rows that do not divide them, of tiles of both sides."""
+    wgrad_case(m, n, k, dt, col=k % 3 == 1, add="apart" if n % 2 else None, seed=9)
