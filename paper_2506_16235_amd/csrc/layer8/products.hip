@@ -313,12 +313,13 @@ int launch_few(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uin
 
 /* Whether k is split over the wavefronts of a workgroup.  Up to 64 rows, unless there are so many rows of b that tiles fill the chip and
  * their ring in LDS keeps more on its way (us, split and in tiles; k = 4096: 1 x 11008 14, 15; 48 x 11008 20, 18; 64 x 4096 14, 14;
- * 16 x 32000 36, 33; 64 x 32000 65, 37).  Beyond that where there are few tiles (512 x 512 x 4096 12, 14; 128 x 768 x 11008 27, 32; 128 x
- * 4096 x 4096 15, 14; 1000 x 1543 x 1024 21, 8). */
-bool by_few(uint64_t m, uint32_t n)
+ * 16 x 32000 36, 33; 64 x 32000 65, 37).  Beyond that where there are few tiles (512 x 512 x 4096 12, 14; 128 x 768 x 11008 27, 32; 171 x 1500 x
+ * 5184 13, 17; 1868 x 179 x 2112, 90 tiles, 8.1, 9.2; 6000 x 64 x 4096, 94, 17, 14; 128 x 4096 x 4096 15, 14) and k is not short (623 x 384 x 517
+ * 4.5, 5.2; 152 x 1939 x 80 5.7, 4.5; 83 x 3060 x 256 5.8, 4.7). */
+bool by_few(uint64_t m, uint32_t n, uint32_t k)
 {
     const uint64_t tiles = ((m + 63) / 64) * ((n + 63) / 64);
-    return m <= 64 ? tiles < (m <= 32 ? 384u : 128u) : m <= 1024 && tiles <= 64;
+    return m <= 64 ? tiles < (m <= 32 ? 384u : 128u) : k > 384 && tiles <= 90;
 }
 
 template <typename T>
@@ -331,16 +332,20 @@ int launch_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb,
      * but 8192 x 5001 x 512 40 -> 56. */
     out.past = m > 64 && large >= 96 && whole_lines(out.c, out.ldc * sizeof(T));
     /* The largest tiles that still give work to most compute units (us by tiles of 256, halved where they are few, 128 and 64: 2048 x 4096 x 4096
-     * 48, 52, 84; 1024 x 4096 x 4096 30, 25, 41; 4096 x 768 x 768 11, 9.3, 10; 1024 x 1536 x 1536 15, 11.5, 10).  Where the weights are read once,
-     * from memory, the ring is twice as long (48 x 11008 x 4096 20.4 -> 18.3). */
+     * 48, 52, 84; 1024 x 4096 x 4096 30, 25, 41; 4096 x 768 x 768 11, 9.3, 10; 1024 x 1536 x 1536 15, 11.5, 10; 6459 x 768 x 2877, 78 of 256, 27,
+     * 31, 37; 5579 x 617 x 1792, 66, 18, 15, 20).  Where k is short, those of 64 as long as the chip holds all of them at a time (5596 x 704 x 97
+     * 8.4, 8.5, 6.2; 279 x 6592 x 640 -, 9.0, 6.6; 4715 x 768 x 768 10.2, 10.0, 11.5; 7819 x 779 x 192 9.6, 10.3, 10.3; 6463 x 896 x 576 11.8,
+     * 11.4, 13.1).  Where the weights are read once, from memory, the ring is twice as long (48 x 11008 x 4096 20.4 -> 18.3).  No side is longer
+     * than the matrix needs (100 x 32000 x 4096 36, 25, 38; 40000 x 128 x 4096 51, 41, 50; 100000 x 64 x 1024 45, 30, 23). */
+    const bool wide = m > 128 && n > 128 && large >= 76;
     if (m <= 64)
         k_product<T, 64, 8><<<(uint32_t)tiles(64), 256, 0, st>>>(a, lda, b, ldb, m, n, k, out);
-    else if (large >= 96)
-        k_product_large<T><<<whole + (large - whole) * 2u, 512, 0, st>>>(a, lda, b, ldb, m, n, k, out, whole);
-    else if (tiles(128) >= 160)
+    else if (n <= 64 || (!wide && tiles(128) < 150) || (k <= 640 && tiles(64) <= 1024))
+        k_product<T, 64, 4><<<(uint32_t)tiles(64), 256, 0, st>>>(a, lda, b, ldb, m, n, k, out);
+    else if (!wide)
         k_product<T, 128, 4><<<(uint32_t)tiles(128), 256, 0, st>>>(a, lda, b, ldb, m, n, k, out);
     else
-        k_product<T, 64, 4><<<(uint32_t)tiles(64), 256, 0, st>>>(a, lda, b, ldb, m, n, k, out);
+        k_product_large<T><<<whole + (large - whole) * 2u, 512, 0, st>>>(a, lda, b, ldb, m, n, k, out, whole);
     return launched();
 }
 
@@ -356,7 +361,7 @@ extern "C" int nsml_q8_matmul(const int8_t *a, uint64_t lda, const float *a_scal
     if (k > NSML_Q8_MAX_COLS || n > MAX_COLS || (m && lda > MAX_LD) || ldb > MAX_LD) return NSML_ECAP;
     if (m == 0) return NSML_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (by_few(m, n)) return launch_few(a, lda, b, ldb, m, n, k, AnyOut{c, ldc, a_scale, b_scale, bias, type}, st);
+    if (by_few(m, n, k)) return launch_few(a, lda, b, ldb, m, n, k, AnyOut{c, ldc, a_scale, b_scale, bias, type}, st);
     if (type == NSML_F32) return launch_product(a, lda, b, ldb, m, n, k, Out<float>{static_cast<float *>(c), ldc, a_scale, b_scale, bias, false}, st);
     if (type == NSML_BF16) return launch_product(a, lda, b, ldb, m, n, k, Out<bf16>{static_cast<bf16 *>(c), ldc, a_scale, b_scale, bias, false}, st);
     return launch_product(a, lda, b, ldb, m, n, k, Out<f16>{static_cast<f16 *>(c), ldc, a_scale, b_scale, bias, false}, st);

@@ -626,3 +626,9 @@ def test_wgrad_large_tiles_in_parts(dt, m, n, k, col, add):
 def test_wgrad_slices(dt, m, n, k):
     """Slices of the rows that do not divide them, of tiles of both sides."""
     wgrad_case(m, n, k, dt, col=k % 3 == 1, add="apart" if n % 2 else None, seed=9)
+
+
+@pytest.mark.parametrize("m,n,k", [(70, 19300, 700), (20000, 61, 700), (20000, 100, 700), (2300, 1177, 71), (130, 2000, 400), (260, 1300, 384), (260, 1300, 385),
+                                   (5600, 704, 97), (279, 6592, 641), (4900, 900, 700), (19000, 150, 650)])
+def test_product_at_more_launches(m, n, k):
+    product_case(m, n, k, TYPES[(m + n + k) % 3], 3, with_b=n % 3 != 0, with_bias=k % 2 == 0)
