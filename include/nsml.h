@@ -297,8 +297,8 @@ int nsml_last_l2norm(nsml_ctx *ctx, double *total, double *per_bucket);
  * NSML_EINVAL: a null pointer, an unknown type, cols == 0, ld < cols, a code matrix or pointer that is not aligned
  * as above; NSML_ECAP: cols beyond the limit named (2^31 - 256 if none is), an ld of a product's or weight gradient's
  * operand beyond 2^22, a result of theirs of more tiles than one launch has (of 256 x 256, about 2^23; for products of up
- * to 64 rows about 2^24 of 64 x 64; for weight gradients with a side up to 128 about 2^24 of 128 x 128); NSML_EHIP: the
- * launch failed.  Buffers of one call must not overlap where one of them is written, unless said otherwise. */
+ * to 64 rows or columns about 2^24 of 64 x 64; for weight gradients with a side up to 128 about 2^24 of 128 x 128);
+ * NSML_EHIP: the launch failed.  Buffers of one call must not overlap where one of them is written, unless said otherwise. */
 
 #define NSML_F32  0
 #define NSML_BF16 1

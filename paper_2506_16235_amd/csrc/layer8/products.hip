@@ -326,7 +326,8 @@ template <typename T>
 int launch_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t m, uint32_t n, uint32_t k, Out<T> out, hipStream_t st)
 {
     const auto tiles = [&](uint64_t s) { return ((m + s - 1) / s) * ((n + s - 1) / s); };
-    if ((m <= 64 ? tiles(64) / 2u : tiles(256)) >= (1u << 23) - 256u) return NSML_ECAP;      /* a launch has fewer than 2^32 threads */
+    /* A launch has fewer than 2^32 threads: 256 for each tile of 64, which results of up to 64 rows or columns take, else at most 512 for each of 256. */
+    if ((m <= 64 ? tiles(64) / 2u : tiles(256)) >= (1u << 23) - 256u || (n <= 64 && tiles(64) >= (1u << 24))) return NSML_ECAP;
     const uint32_t large = (uint32_t)tiles(256), rest = large % 256u, whole = rest <= 128u ? large - rest : large;
     /* Large results go past the caches, where the operands are read from, if their rows are whole lines: 8192 x 11008 x 1024 131 -> 124 us,
      * but 8192 x 5001 x 512 40 -> 56. */

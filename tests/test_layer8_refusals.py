@@ -174,3 +174,9 @@ def test_results_of_more_tiles_than_a_launch_has():
     for m, n in ((1, 1 << 30), (64, (1 << 30) - 32768 + 1), (1 << 31, 1), (1 << 29, 1024)):
         refused(L.nsml_q8_matmul(P, 16, P, P, 16, P, None, m, n, 16, P, 1, n, None), nsml.ECAP)
     refused(L.nsml_ckpt8_wgrad(P, 1, 1 << 21, ck(ldq=1 << 21, lde=1 << 16), None, 3, 1 << 21, 1 << 21, None, P, 1 << 21, P, 1 << 40, None), nsml.ECAP)
+
+
+@pytest.mark.parametrize("m,n", [(1 << 30, 1), (1 << 30, 64), ((1 << 30) - 63, 64), ((1 << 31) - 65800, 1), ((1 << 31) - 65800, 64)])
+def test_tall_products_of_few_columns_beyond_a_launch(m, n):
+    """Up to 64 columns take tiles of 64 rows however many rows there are: 2^24 of them have 2^32 threads."""
+    refused(L.nsml_q8_matmul(P, 16, P, P, 16, P, None, m, n, 16, P, 1, n, None), nsml.ECAP)
