@@ -180,3 +180,9 @@ def test_results_of_more_tiles_than_a_launch_has():
 def test_tall_products_of_few_columns_beyond_a_launch(m, n):
     """Up to 64 columns take tiles of 64 rows however many rows there are: 2^24 of them have 2^32 threads."""
     refused(L.nsml_q8_matmul(P, 16, P, P, 16, P, None, m, n, 16, P, 1, n, None), nsml.ECAP)
+
+
+@pytest.mark.parametrize("n,k", [(1 << 20, 1 << 19), ((1 << 19) + 1, 1 << 20), (1 << 20, (1 << 20) - 256)])
+def test_weight_gradients_beyond_a_launch(n, k):
+    """2^23 tiles of 256 have 2^32 threads."""
+    refused(L.nsml_ckpt8_wgrad(P, 1, n, ck(ldq=k, lde=k // 32), None, 3, n, k, None, P, k, P, 1 << 40, None), nsml.ECAP)
