@@ -1,0 +1,77 @@
+"""The 8-bit layer at the ends of binary32's range and over the whole range of its exponential, against 64 bits.
+
+u = 2^-24.  The sigmoid is the GPU's exponential of two and reciprocal, documented as within a unit in the last place (2u) each, a factor of two
+roundings (2u) and a fused sum (u): 7u.  Its results below 2^-126 may be 0."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2506_16235_amd import binding as nsml
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+u = 2.0 ** -24
+LEAST = 2.0 ** -126
+SIGMOID = 7 * u
+
+
+def f64(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def sigma(g):
+    with np.errstate(over="ignore"):
+        return np.where(g >= 0, 1 / (1 + np.exp(-np.abs(g))), np.exp(-np.abs(g)) / (1 + np.exp(-np.abs(g))))
+
+
+def gates(top, rows=64, k=1024, seed=0):
+    """A checkpoint of values up to `top` of both signs, and what it holds."""
+    g = torch.Generator()
+    g.manual_seed(seed)
+    c = nsml.ckpt8_pack(((torch.rand(rows, k, generator=g) * 2 - 1) * top).to(DEV))
+    return c, f64(nsml.ckpt8_unpack(c))
+
+
+@pytest.mark.parametrize("top", [0.5, 3.0, 8.0, 20.0, 40.0, 87.0, 300.0])
+def test_sigmoid_of_binary32(top):
+    """dup = da * gate * s with da = 1: one rounding behind the sigmoid.  dgate = da * up * s * (1 + gate * (1 - s)) with up = 1."""
+    c, g = gates(top, seed=int(top))
+    one = torch.ones(g.shape, device=DEV)
+    dg, du = nsml.swiglu_backward(one, c, nsml.ckpt8_pack(one))
+    s = sigma(g)
+    err = np.abs(f64(du) - g * s)
+    assert (err <= (SIGMOID + u) * np.abs(g) * s + np.abs(g) * LEAST).all(), f"{np.max(err / (np.abs(g) * s + 1e-300)) / u:.1f} u"
+    size = 1 + np.abs(g) * (1 - s)
+    lim = s * (SIGMOID * size + np.abs(g) * (SIGMOID * s + u) + 2 * u * size)
+    assert (np.abs(f64(dg) - s * (1 + g * (1 - s))) <= lim + size * LEAST).all()
+
+
+def test_gradient_at_large_gates():
+    """What lies beyond the exponential's range: gradients of a step."""
+    g = torch.tensor([[-2.0 ** 100, -2.0 ** 20, -256.0, 256.0, 2.0 ** 20, 2.0 ** 100] + [0.0] * 26]).repeat(6, 1)
+    g = torch.where(torch.eye(6, 32) > 0, g, torch.zeros(6, 32))            # one a block, held exactly
+    c, one = nsml.ckpt8_pack(g.to(DEV)), torch.ones(6, 32, device=DEV)
+    dg, du = nsml.swiglu_backward(one, c, nsml.ckpt8_pack(one))
+    d = torch.arange(6)
+    assert (dg[d, d].cpu() == torch.tensor([0.0, 0, 0, 1, 1, 1])).all()
+    assert torch.equal(du[d, d].cpu().abs(), torch.where(g[d, d] > 0, g[d, d], torch.zeros(6)))
+    assert (dg[0, 10:] == 0.5).all() and (du[0, 10:] == 0).all()
+
+
+@pytest.mark.parametrize("top", [1.0, 8.0, 20.0, 60.0])
+def test_codes_of_the_activation(top):
+    """a = gate * s * up, s without that factor: the product with log2 e off by u of it and its constant by 0.22 u, so 1.25 |gate| u, instructions and a
+    sum 5u; two roundings behind it; a row's scale one more, its quotients three more."""
+    g = torch.Generator()
+    g.manual_seed(3)
+    gate, up = -torch.rand(33, 1500, generator=g) * top, torch.randn(33, 1500, generator=g)
+    gate[:, ::97] *= -1
+    gate[1] = -top                                  # a row whose absmax stands far below
+    o = nsml.swiglu_q8(gate.to(DEV), up.to(DEV))
+    a = f64(gate) * sigma(f64(gate)) * f64(up)
+    rel = (7 + 1.25 * np.abs(f64(gate))) * u
+    top_a = np.abs(a).max(1)
+    at = rel.max(1)                                 # whichever came out on top
+    assert (np.abs(f64(o.a.scale) - top_a / 127) <= (at + u) * top_a / 127).all()
+    exact = a * 127 / top_a[:, None]
+    assert (np.abs(o.a.q.cpu().numpy() - exact) <= 0.5 + np.abs(exact) * (rel + at[:, None] + 2 * u)).all()
