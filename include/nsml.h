@@ -351,7 +351,9 @@ int nsml_ckpt8_wgrad(const void *dy, int type, uint64_t lddy, const nsml_ckpt8 *
  *   h = x + residual (type, rounded; both NULL: h is x)       rstd = 1 / sqrt(mean of h^2 over the row + eps)
  *   (q, scale) = rows of gamma * h * rstd                     xhat = checkpoint of h * rstd (or NULL)
  * gamma: dev, float[cols], or NULL for 1.  rstd: dev, out, float[rows].  Codes do not depend on how the mean was rounded:
- * they are those of gamma * h, and rstd goes into the scale.  cols <= NSML_NORM_MAX_COLS. */
+ * they are those of gamma * h, and rstd goes into the scale: the absmax of gamma * h is what has to be 2^-112 or more for codes other than 0,
+ * and finite.  h^2 may leave binary32's range; rstd ends at its largest value, so that a row of zeros without eps has scale 0, a
+ * checkpoint of zeros and, where dy is 0, a gradient of 0.  cols <= NSML_NORM_MAX_COLS. */
 int nsml_rmsnorm_q8(const void *x, uint64_t ldx, const void *residual, uint64_t ldr, const float *gamma, float eps,
                     int type, uint64_t rows, uint32_t cols, void *h, uint64_t ldh, int8_t *q, uint64_t ldq,
                     float *scale, float *rstd, const nsml_ckpt8 *xhat, void *stream);

@@ -7,6 +7,8 @@
  */
 #include "layer8.hpp"
 
+#include <cfloat>
+
 namespace {
 
 /* ---------------------------------------------------------------- reductions */
@@ -32,8 +34,8 @@ __device__ __forceinline__ uint32_t sum_of(uint32_t a, uint32_t b) { return to_b
 /* ---------------------------------------------------------------- rows that are coded as a whole */
 
 /* T threads hold a row, V times eight neighbours each; V == 0: rows wider than registers hold are read twice.
- * OP: load() gives the values to code and adds to the row's sum, done() gets the sum and the row's code,
- * store() writes beside the codes.  SHORT: two times eight per thread at most. */
+ * OP: load() gives the values to code and adds to the row's sum (SUMS; again() once more, in another unit), done() gets the sum and
+ * the row's code, store() writes beside the codes.  SHORT: two times eight per thread at most. */
 template <int T, int V, typename OP>
 __global__ void __launch_bounds__(T < 256 ? 256 : T) k_rows(OP op, uint64_t rows, uint32_t cols)
 {
@@ -70,8 +72,31 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) k_rows(OP op, uint64_t rows
                 if (OP::SUMS) sum += from_bits(part[turn][1][i]);
             }
         }
+        if constexpr (OP::SUMS) {
+            /* The same for all threads of a row. */
+            if (__builtin_expect(op.left_range(sum), 0)) {
+                const float unit = sum > 1.0f ? 0x1p-75f : 0x1p+75f;
+                uint32_t thread = threadIdx.x;
+                asm volatile("" : "+v"(thread));     /* nothing of this is kept in registers where it is not needed */
+                sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < N; i++) sum = op.again(reg[i], unit, sum);
+                sum = from_bits(wave_all(to_bits(sum), sum_of));
+                if (W > 1) {
+                    wg_sync();               /* the first sum's parts have been read */
+                    if (thread % 64 == 0) part[turn][1][thread / 64] = to_bits(sum);
+                    wg_sync();
+                    sum = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < W; i++) sum += from_bits(part[turn][1][i]);
+                }
+                op.mean(sum, cols, unit);
+            } else {
+                op.mean(sum, cols, 1.0f);
+            }
+        }
         const RowCode rc = row_code(m);
-        op.done(row, t == 0, sum, rc, cols);
+        op.done(row, t == 0, rc);
         if (V) {
 #pragma unroll
             for (int i = 0; i < N; i++) {
@@ -113,8 +138,8 @@ template <typename OP> int launch_rows(const OP &op, uint64_t rows, uint32_t col
     if (cols <= 8192) return go_rows<512, 2>(op, rows, cols, st);
     if (cols <= 12288) return go_rows<OP::SHORT ? 768 : 512, OP::SHORT ? 2 : 3>(op, rows, cols, st);
     if (cols <= 16384) return go_rows<OP::SHORT ? 1024 : 512, OP::SHORT ? 2 : 4>(op, rows, cols, st);
-    if (cols <= 32768) return go_rows<1024, 4>(op, rows, cols, st);
-    return go_rows<1024, 0>(op, rows, cols, st);
+    if constexpr (OP::SUMS) return go_rows<1024, 4>(op, rows, cols, st);          /* up to 32768 columns */
+    else return cols <= 32768 ? go_rows<1024, 4>(op, rows, cols, st) : go_rows<1024, 0>(op, rows, cols, st);
 }
 
 template <typename T> struct OpRows {
@@ -135,7 +160,7 @@ template <typename T> struct OpRows {
         }
         m = max8(r.t, m);
     }
-    __device__ __forceinline__ void done(uint64_t row, bool first, float, RowCode rc, uint32_t) const
+    __device__ __forceinline__ void done(uint64_t row, bool first, RowCode rc) const
     {
         if (first) scale[row] = rc.scale;
     }
@@ -178,9 +203,25 @@ template <typename T> struct OpNorm {
         }
         m = max8(g.t, m);
     }
-    __device__ __forceinline__ void done(uint64_t row, bool first, float sum, RowCode rc, uint32_t cols)
+    /* Whether the sum of squares has left binary32's range, or squares that count may have: they are then added once more in a unit, a
+     * power of two, that brings them back (a sum below 2^-75 to one below 2^75; an infinity among the values stays one). */
+    __device__ __forceinline__ bool left_range(float sum) const { return sum > FLT_MAX || (sum < 0x1p-75f && eps < 0x1p-90f); }
+    __device__ __forceinline__ float again(const Reg &g, float unit, float sum) const
     {
-        r = rsqrtf(sum / (float)cols + eps);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float v = g.h[i] * unit;
+            sum = __builtin_fmaf(v, v, sum);
+        }
+        return sum;
+    }
+    __device__ __forceinline__ void mean(float sum, uint32_t cols, float unit)
+    {
+        r = rsqrtf(sum / (float)cols + eps * unit * unit) * unit;
+        if (r > FLT_MAX) r = FLT_MAX;        /* a row of zeros without eps: what it is multiplied by stays 0 */
+    }
+    __device__ __forceinline__ void done(uint64_t row, bool first, RowCode rc) const
+    {
         if (first) {
             rstd[row] = r;
             scale[row] = rc.scale * r;
@@ -232,7 +273,7 @@ template <typename T> struct OpGlu {
         for (int i = 0; i < 8; i++) r.t[i] = g[i] * sigmoid_rough(g[i]) * u[i];
         m = max8(r.t, m);
     }
-    __device__ __forceinline__ void done(uint64_t row, bool first, float, RowCode rc, uint32_t) const
+    __device__ __forceinline__ void done(uint64_t row, bool first, RowCode rc) const
     {
         if (first) scale[row] = rc.scale;
     }

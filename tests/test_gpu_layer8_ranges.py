@@ -75,3 +75,64 @@ def test_codes_of_the_activation(top):
     assert (np.abs(f64(o.a.scale) - top_a / 127) <= (at + u) * top_a / 127).all()
     exact = a * 127 / top_a[:, None]
     assert (np.abs(o.a.q.cpu().numpy() - exact) <= 0.5 + np.abs(exact) * (rel + at[:, None] + 2 * u)).all()
+
+
+@pytest.mark.parametrize("k", [1, 40, 333, 1000, 1777, 4000, 8000, 20000, 32768])
+def test_norm_of_rows_whose_squares_leave_the_range(k):
+    """rstd: a sum of k squares (each off by 2u, added in an order with k u at most), a division, a sum, a root of two units, two exact products."""
+    g = torch.Generator()
+    g.manual_seed(k)
+    powers = [0, 60, 64, 70, 100, 120, -20, -50, -60, -64, -80, -100]
+    x = torch.stack([torch.randn(k, generator=g).clamp(-4, 4) * 2.0 ** p for p in powers])
+    x[:, 0] = torch.tensor([2.0 ** p for p in powers])
+    res = torch.zeros_like(x)
+    o = nsml.rmsnorm_q8(x.to(DEV), None, 0.0, residual=res.to(DEV), checkpoint=True)
+    h = f64(x)
+    rstd = 1 / np.sqrt((h * h).mean(1))
+    tol = (8 + np.sqrt(k)) * u
+    assert (f64(o.h) == h).all()
+    assert (np.abs(f64(o.rstd) - rstd) <= tol * rstd).all()
+    top = np.abs(h).max(1)
+    assert (np.abs(f64(o.y.scale) - top / 127 * rstd) <= (tol + 4 * u) * top / 127 * rstd).all()
+    exact = h * 127 / top[:, None]
+    assert (np.abs(o.y.q.cpu().numpy() - exact) <= 0.5 + 127 * 4 * u).all()
+    v, got = h * rstd[:, None], f64(nsml.ckpt8_unpack(o.xhat))
+    most = np.stack([np.abs(v[:, i // 32 * 32:i // 32 * 32 + 32]).max(1) for i in range(0, k, 32)], 1).repeat(32, 1)[:, :k]
+    step = np.exp2(np.maximum(np.floor(np.log2(most)) - 6, -126))
+    # half a step; a value that rounds to 128 steps is held to 127; a block next to a power of two may take the step below or above
+    assert (np.abs(got - v) <= 1.001 * step).all()
+    # with an eps that counts, and in the range's middle, as ever
+    eps = 1e-5
+    rstd = 1 / np.sqrt((h * h).mean(1) + eps)
+    o = nsml.rmsnorm_q8(x.to(DEV), None, eps)
+    assert (np.abs(f64(o.rstd) - rstd) <= tol * rstd).all()
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16, torch.float16], ids=["f32", "bf16", "f16"])
+@pytest.mark.parametrize("k", [1, 48, 777, 2000, 4096, 9000])
+def test_rows_of_zeros_without_eps(dt, k):
+    """Padding stays padding: forward, and backward for a gradient of zeros; other rows are what they are without it."""
+    g = torch.Generator()
+    g.manual_seed(k)
+    x = torch.randn(6, k, generator=g).to(dt)
+    x[:, 0] = 1
+    alone = x.clone()
+    x[1], x[4] = 0, 0
+    o, p = (nsml.rmsnorm_q8(t.to(DEV), None, 0.0, checkpoint=True) for t in (x, alone))
+    z, other = [1, 4], [0, 2, 3, 5]
+    assert (o.y.scale[z] == 0).all() and (o.y.q[z] == 0).all() and (nsml.q8_values(o.y)[z] == 0).all()
+    assert (nsml.ckpt8_unpack(o.xhat)[z] == 0).all()
+    assert torch.equal(o.y.q[other], p.y.q[other]) and torch.equal(o.y.scale[other], p.y.scale[other]) and torch.equal(o.rstd[other], p.rstd[other])
+    dy = torch.randn(6, k, generator=g).to(dt)
+    dy[z] = 0
+    dx, dgamma = nsml.rmsnorm_backward(dy.to(DEV), o.xhat, o.rstd)
+    assert (dx[z] == 0).all() and torch.isfinite(dx[other]).all() and torch.isfinite(dgamma).all()
+
+
+def test_norm_of_infinities_is_still_seen():
+    x = torch.full((4, 100), 2.0 ** 80)
+    x[1, 7], x[2, 99], x[3, 0] = float("inf"), float("nan"), float("-inf")
+    o = nsml.rmsnorm_q8(x.to(DEV), None, 0.0, checkpoint=True)
+    y, v = nsml.q8_values(o.y).cpu(), nsml.ckpt8_unpack(o.xhat).cpu()
+    assert torch.isnan(y[1:]).all() and (y[0] == y[0, 0]).all() and abs(float(y[0, 0]) - 1) < 1e-6
+    assert torch.isnan(v[1, :32]).all() and torch.isnan(v[2]).all() and torch.isnan(v[3, :32]).all() and (abs(v[0] - 1) <= 2.0 ** -6).all()
