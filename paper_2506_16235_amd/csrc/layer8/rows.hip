@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) k_rows(OP op, uint64_t rows
                     if (thread % 64 == 0) part[turn][1][thread / 64] = to_bits(sum);
                     wg_sync();
                     sum = 0.0f;
-#pragma unroll
+#pragma unroll 1
                     for (int i = 0; i < W; i++) sum += from_bits(part[turn][1][i]);
                 }
                 op.mean(sum, cols, unit);
