@@ -295,10 +295,11 @@ int nsml_last_l2norm(nsml_ctx *ctx, double *total, double *per_bucket);
  *   code matrices   16-byte aligned, ld a multiple of 16; the bytes of a row up to the next multiple of 16
  *             belong to it (their contents are never used as values, and may be overwritten)
  * NSML_EINVAL: a null pointer, an unknown type, cols == 0, ld < cols, a code matrix or pointer that is not aligned
- * as above; NSML_ECAP: cols beyond the limit named (2^31 - 256 if none is), an ld of a product's or weight gradient's
+ * as above, buffers that share bytes where one of them is written (unless said otherwise; parts of one matrix side by side share none);
+ * NSML_ECAP: cols beyond the limit named (2^31 - 256 if none is), an ld of a product's or weight gradient's
  * operand beyond 2^22, a result of theirs of more tiles than one launch has (of 256 x 256, about 2^23; for products of up
  * to 64 rows or columns about 2^24 of 64 x 64; for weight gradients with a side up to 128 about 2^24 of 128 x 128);
- * NSML_EHIP: the launch failed.  Buffers of one call must not overlap where one of them is written, unless said otherwise. */
+ * NSML_EHIP: the launch failed. */
 
 #define NSML_F32  0
 #define NSML_BF16 1
@@ -350,7 +351,7 @@ int nsml_ckpt8_wgrad(const void *dy, int type, uint64_t lddy, const nsml_ckpt8 *
 /* Root-mean-square norm with the residual's addition, in 8 bits:
  *   h = x + residual (type, rounded; both NULL: h is x)       rstd = 1 / sqrt(mean of h^2 over the row + eps)
  *   (q, scale) = rows of gamma * h * rstd                     xhat = checkpoint of h * rstd (or NULL)
- * gamma: dev, float[cols], or NULL for 1.  rstd: dev, out, float[rows].  Codes do not depend on how the mean was rounded:
+ * gamma: dev, float[cols], or NULL for 1.  rstd: dev, out, float[rows].  h may be x or residual itself.  Codes do not depend on how the mean was rounded:
  * they are those of gamma * h, and rstd goes into the scale: the absmax of gamma * h is what has to be 2^-112 or more for codes other than 0,
  * and finite.  h^2 may leave binary32's range; rstd ends at its largest value, so that a row of zeros without eps has scale 0, a
  * checkpoint of zeros and, where dy is 0, a gradient of 0.  cols <= NSML_NORM_MAX_COLS. */
@@ -361,6 +362,7 @@ int nsml_rmsnorm_q8(const void *x, uint64_t ldx, const void *residual, uint64_t 
  *   dx = rstd * (g - xhat * mean(g * xhat)) + dres            gradient of x and of residual; dres (type) or NULL:
  *                                                             what reaches h by the residual stream
  *   dgamma[i] = sum over rows of dy * xhat                    dev, out, float[cols], or NULL
+ * dx may be dy or dres itself.
  * work: dev, 16-byte aligned, nsml_rmsnorm_backward_work(rows, cols) bytes, needed for dgamma.  rows == 0: dgamma = 0. */
 uint64_t nsml_rmsnorm_backward_work(uint64_t rows, uint32_t cols);
 int nsml_rmsnorm_backward(const void *dy, uint64_t lddy, const nsml_ckpt8 *xhat, const float *rstd, const float *gamma,
@@ -373,7 +375,7 @@ int nsml_swiglu_q8(const void *gate, uint64_t ldg, const void *up, uint64_t ldu,
                    int8_t *q, uint64_t ldq, float *scale, const nsml_ckpt8 *gate_ckpt, const nsml_ckpt8 *up_ckpt,
                    const nsml_ckpt8 *act_ckpt, void *stream);
 /* Its gradient from the checkpoints: s = 1 / (1 + exp(-gate)), dup = da * gate * s,
- * dgate = da * up * s * (1 + gate * (1 - s)).  dgate and dup may be parts of one matrix. */
+ * dgate = da * up * s * (1 + gate * (1 - s)).  dgate and dup may be parts of one matrix, and one of them da itself. */
 int nsml_swiglu_backward(const void *da, uint64_t ldda, const nsml_ckpt8 *gate, const nsml_ckpt8 *up, int type,
                          uint64_t rows, uint32_t cols, void *dgate, uint64_t lddg, void *dup, uint64_t lddu, void *stream);
 

@@ -8,6 +8,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <initializer_list>
 
 #include "nsml.h"
 
@@ -228,6 +229,54 @@ inline bool bad_ckpt(const nsml_ckpt8 *k, uint32_t cols)
     return !k || !k->e || k->lde < (cols + 31u) / 32u || bad_codes(k->q, k->ldq, cols);
 }
 inline Ckpt ckpt_of(const nsml_ckpt8 *k) { return k ? Ckpt{k->q, k->e, k->ldq, k->lde} : Ckpt{nullptr, nullptr, 0, 0}; }
+
+/* The bytes of a matrix: `rows` times `width`, `pitch` from row to row. */
+struct Area { uintptr_t at; uint64_t rows, pitch, width; };
+inline Area area(const void *p, uint64_t rows, uint64_t pitch, uint64_t width) { return {reinterpret_cast<uintptr_t>(p), p ? rows : 0, pitch, width}; }
+inline Area area(const void *p, int type, uint64_t rows, uint64_t ld, uint32_t cols) { return area(p, rows, ld * type_bytes(type), (uint64_t)cols * type_bytes(type)); }
+inline Area floats(const float *p, uint64_t n) { return area(p, 1, n * 4u, n * 4u); }
+inline Area codes_area(const int8_t *p, uint64_t rows, uint64_t ld, uint32_t cols) { return area(p, rows, ld, ((uint64_t)cols + 15u) / 16u * 16u); }
+inline Area exps_area(const nsml_ckpt8 *k, uint64_t rows, uint32_t cols) { return area(k ? k->e : nullptr, rows, k ? k->lde : 0, (cols + 31u) / 32u); }
+inline Area codes_area(const nsml_ckpt8 *k, uint64_t rows, uint32_t cols) { return codes_area(k ? k->q : nullptr, rows, k ? k->ldq : 0, cols); }
+/* Whether two matrices have a byte in common.  Matrices side by side in one (the same pitch) do not. */
+inline bool meet(Area a, Area b)
+{
+    if (a.rows == 0 || b.rows == 0 || a.width == 0 || b.width == 0) return false;
+    if (b.at < a.at) {
+        const Area c = a;
+        a = b, b = c;
+    }
+    if (b.at >= a.at + (a.rows - 1) * a.pitch + a.width) return false;
+    if (a.rows == 1) return true;
+    const uint64_t in = (b.at - a.at) % a.pitch;
+    if (in < a.width) return true;
+    if (b.rows == 1 || b.pitch == a.pitch) return in + b.width > a.pitch;        /* the row of a behind it is there: b begins before a ends */
+    uint64_t i = (b.at - a.at) / a.pitch + 1, j = 0;
+    while (i < a.rows && j < b.rows) {
+        const uintptr_t x = a.at + i * a.pitch, y = b.at + j * b.pitch;
+        if (x + a.width <= y) i++;
+        else if (y + b.width <= x) j++;
+        else return true;
+    }
+    return false;
+}
+/* Whether one that is written meets another, or one that is read. */
+inline bool clash(std::initializer_list<Area> written, std::initializer_list<Area> read)
+{
+    for (const Area *w = written.begin(); w != written.end(); w++) {
+        for (const Area *o = written.begin(); o != w; o++)
+            if (meet(*w, *o)) return true;
+        for (const Area &r : read)
+            if (meet(*w, r)) return true;
+    }
+    return false;
+}
+/* What is read, but nothing where it is the very matrix that is written: where every thread reads an element before it writes it. */
+inline Area apart(Area read, const Area &written)
+{
+    if (read.at == written.at && read.rows == written.rows && read.width == written.width && (read.pitch == written.pitch || read.rows == 1)) read.rows = 0;
+    return read;
+}
 inline int launched() { return hipGetLastError() == hipSuccess ? NSML_OK : NSML_EHIP; }
 template <typename T> Mat<T> mat(void *p, uint64_t ld) { return {static_cast<T *>(p), ld}; }
 template <typename T> Mat<const T> mat(const void *p, uint64_t ld) { return {static_cast<const T *>(p), ld}; }

@@ -322,12 +322,17 @@ bool by_few(uint64_t m, uint32_t n, uint32_t k)
     return m <= 64 ? tiles < (m <= 32 ? 384u : 128u) : k > 384 && tiles <= 90;
 }
 
+/* A launch has fewer than 2^32 threads: 256 for each tile of 64, which results of up to 64 rows or columns take, else at most 512 for each of 256. */
+bool beyond_a_launch(uint64_t m, uint32_t n)
+{
+    const auto tiles = [&](uint64_t s) { return ((m + s - 1) / s) * ((n + s - 1) / s); };
+    return (m <= 64 ? tiles(64) / 2u : tiles(256)) >= (1u << 23) - 256u || (n <= 64 && tiles(64) >= (1u << 24));
+}
+
 template <typename T>
 int launch_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uint64_t m, uint32_t n, uint32_t k, Out<T> out, hipStream_t st)
 {
     const auto tiles = [&](uint64_t s) { return ((m + s - 1) / s) * ((n + s - 1) / s); };
-    /* A launch has fewer than 2^32 threads: 256 for each tile of 64, which results of up to 64 rows or columns take, else at most 512 for each of 256. */
-    if ((m <= 64 ? tiles(64) / 2u : tiles(256)) >= (1u << 23) - 256u || (n <= 64 && tiles(64) >= (1u << 24))) return NSML_ECAP;
     const uint32_t large = (uint32_t)tiles(256), rest = large % 256u, whole = rest <= 128u ? large - rest : large;
     /* Large results go past the caches, where the operands are read from, if their rows are whole lines: 8192 x 11008 x 1024 131 -> 124 us,
      * but 8192 x 5001 x 512 40 -> 56. */
@@ -359,8 +364,10 @@ extern "C" int nsml_q8_matmul(const int8_t *a, uint64_t lda, const float *a_scal
     if (n == 0 || k == 0 || bad_type(type) || bad_codes(b, ldb, k) || (b_scale && bad_f32(b_scale)) || (bias && bad_f32(bias)) ||
         (m && (bad_codes(a, lda, k) || bad_f32(a_scale) || bad_mat(c, type, ldc, n))))
         return NSML_EINVAL;
-    if (k > NSML_Q8_MAX_COLS || n > MAX_COLS || (m && lda > MAX_LD) || ldb > MAX_LD) return NSML_ECAP;
+    if (k > NSML_Q8_MAX_COLS || n > MAX_COLS || (m && lda > MAX_LD) || ldb > MAX_LD || beyond_a_launch(m, n)) return NSML_ECAP;
     if (m == 0) return NSML_OK;
+    if (clash({area(c, type, m, ldc, n)}, {codes_area(a, m, lda, k), codes_area(b, n, ldb, k), floats(a_scale, m), floats(b_scale, n), floats(bias, n)}))
+        return NSML_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (by_few(m, n, k)) return launch_few(a, lda, b, ldb, m, n, k, AnyOut{c, ldc, a_scale, b_scale, bias, type}, st);
     if (type == NSML_F32) return launch_product(a, lda, b, ldb, m, n, k, Out<float>{static_cast<float *>(c), ldc, a_scale, b_scale, bias, false}, st);

@@ -530,6 +530,7 @@ int nsml_q8_rows(const void *x, int type, uint64_t ldx, uint64_t rows, uint32_t 
         (rows && (bad_mat(x, type, ldx, cols) || bad_codes(q, ldq, cols) || bad_f32(scale))))
         return NSML_EINVAL;
     if (cols > NSML_Q8_MAX_COLS) return NSML_ECAP;
+    if (clash({codes_area(q, rows, ldq, cols), floats(scale, rows)}, {area(x, type, rows, ldx, cols), floats(col_scale, cols)})) return NSML_EINVAL;
     return by_type(type, [&](auto v) {
         using T = decltype(v);
         return launch_rows(OpRows<T>{mat<T>(x, ldx), col_scale, mat<int8_t>((void *)q, ldq), scale}, rows, cols, (hipStream_t)stream);
@@ -542,6 +543,7 @@ int nsml_q8_values(const int8_t *q, uint64_t ldq, const float *scale, uint64_t r
     if (cols == 0 || bad_type(type) || (rows && (bad_codes(q, ldq, cols) || (scale && bad_f32(scale)) || bad_mat(out, type, ldo, cols))))
         return NSML_EINVAL;
     if (cols > MAX_COLS) return NSML_ECAP;
+    if (clash({area(out, type, rows, ldo, cols)}, {codes_area(q, rows, ldq, cols), floats(scale, rows)})) return NSML_EINVAL;
     return by_type(type, [&](auto v) {
         using T = decltype(v);
         return launch_each(OpValues<T>{mat<int8_t>((const void *)q, ldq), scale, mat<T>(out, ldo)}, rows, cols, (hipStream_t)stream);
@@ -552,6 +554,7 @@ int nsml_ckpt8_pack(const void *x, int type, uint64_t ldx, uint64_t rows, uint32
 {
     if (cols == 0 || bad_type(type) || (rows && (bad_mat(x, type, ldx, cols) || bad_ckpt(out, cols)))) return NSML_EINVAL;
     if (cols > MAX_COLS) return NSML_ECAP;
+    if (clash({codes_area(out, rows, cols), exps_area(out, rows, cols)}, {area(x, type, rows, ldx, cols)})) return NSML_EINVAL;
     return by_type(type, [&](auto v) {
         using T = decltype(v);
         return launch_each(OpPack<T>{mat<T>(x, ldx), ckpt_of(out)}, rows, cols, (hipStream_t)stream);
@@ -562,6 +565,7 @@ int nsml_ckpt8_unpack(const nsml_ckpt8 *x, uint64_t rows, uint32_t cols, void *o
 {
     if (cols == 0 || bad_type(type) || (rows && (bad_ckpt(x, cols) || bad_mat(out, type, ldo, cols)))) return NSML_EINVAL;
     if (cols > MAX_COLS) return NSML_ECAP;
+    if (clash({area(out, type, rows, ldo, cols)}, {codes_area(x, rows, cols), exps_area(x, rows, cols)})) return NSML_EINVAL;
     return by_type(type, [&](auto v) {
         using T = decltype(v);
         return launch_each(OpUnpack<T>{ckpt_of(x), mat<T>(out, ldo)}, rows, cols, (hipStream_t)stream);
@@ -578,6 +582,10 @@ int nsml_rmsnorm_q8(const void *x, uint64_t ldx, const void *residual, uint64_t 
                   bad_codes(q, ldq, cols) || bad_f32(scale) || bad_f32(rstd) || (xhat && bad_ckpt(xhat, cols)))))
         return NSML_EINVAL;
     if (cols > NSML_NORM_MAX_COLS) return NSML_ECAP;
+    const Area sum = area(h, type, rows, ldh, cols);
+    if (clash({sum, codes_area(q, rows, ldq, cols), floats(scale, rows), floats(rstd, rows), codes_area(xhat, rows, cols), exps_area(xhat, rows, cols)},
+              {apart(area(x, type, rows, ldx, cols), sum), apart(area(residual, type, rows, ldr, cols), sum), floats(gamma, cols)}))
+        return NSML_EINVAL;
     return by_type(type, [&](auto v) {
         using T = decltype(v);
         return launch_rows(OpNorm<T>{mat<T>(x, ldx), mat<T>(residual, ldr), gamma, eps, mat<T>(h, ldh),
@@ -606,6 +614,11 @@ int nsml_rmsnorm_backward(const void *dy, uint64_t lddy, const nsml_ckpt8 *xhat,
         if (rows && (!work || !at_multiple(work, 16) || work_bytes < nsml_rmsnorm_backward_work(rows, cols))) return NSML_EINVAL;
         part = static_cast<float *>(work);
     }
+    const Area out = area(dx, type, rows, lddx, cols);
+    if (clash({out, floats(dgamma, cols), area(part, 1, 0, nsml_rmsnorm_backward_work(rows, cols))},
+              {apart(area(dy, type, rows, lddy, cols), out), apart(area(dres, type, rows, lddres, cols), out), codes_area(xhat, rows, cols),
+               exps_area(xhat, rows, cols), floats(rstd, rows), floats(gamma, cols)}))
+        return NSML_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (rows) {
         const int rc = by_type(type, [&](auto v) {
@@ -631,6 +644,10 @@ int nsml_swiglu_q8(const void *gate, uint64_t ldg, const void *up, uint64_t ldu,
                   (gate_ckpt && bad_ckpt(gate_ckpt, cols)) || (up_ckpt && bad_ckpt(up_ckpt, cols)) || (act_ckpt && bad_ckpt(act_ckpt, cols)))))
         return NSML_EINVAL;
     if (cols > NSML_Q8_MAX_COLS) return NSML_ECAP;
+    if (clash({codes_area(q, rows, ldq, cols), floats(scale, rows), codes_area(gate_ckpt, rows, cols), exps_area(gate_ckpt, rows, cols),
+               codes_area(up_ckpt, rows, cols), exps_area(up_ckpt, rows, cols), codes_area(act_ckpt, rows, cols), exps_area(act_ckpt, rows, cols)},
+              {area(gate, type, rows, ldg, cols), area(up, type, rows, ldu, cols)}))
+        return NSML_EINVAL;
     return by_type(type, [&](auto v) {
         using T = decltype(v);
         return launch_rows(OpGlu<T>{mat<T>(gate, ldg), mat<T>(up, ldu), mat<int8_t>((void *)q, ldq), scale, ckpt_of(gate_ckpt),
@@ -646,6 +663,10 @@ int nsml_swiglu_backward(const void *da, uint64_t ldda, const nsml_ckpt8 *gate, 
                   bad_mat(dgate, type, lddg, cols) || bad_mat(dup, type, lddu, cols))))
         return NSML_EINVAL;
     if (cols > MAX_COLS) return NSML_ECAP;
+    const Area g = area(dgate, type, rows, lddg, cols), u = area(dup, type, rows, lddu, cols);
+    if (clash({g, u}, {apart(apart(area(da, type, rows, ldda, cols), g), u), codes_area(gate, rows, cols), exps_area(gate, rows, cols),
+                       codes_area(up, rows, cols), exps_area(up, rows, cols)}))
+        return NSML_EINVAL;
     return by_type(type, [&](auto v) {
         using T = decltype(v);
         return launch_each(OpGluBack<T>{mat<T>(da, ldda), ckpt_of(gate), ckpt_of(up), mat<T>(dgate, lddg), mat<T>(dup, lddu)}, rows, cols,

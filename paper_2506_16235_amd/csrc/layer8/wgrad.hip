@@ -370,6 +370,10 @@ int nsml_ckpt8_wgrad(const void *dy, int type, uint64_t lddy, const nsml_ckpt8 *
     const Shape s = shape_of(rows, n, k, type);
     /* A launch has fewer than 2^32 threads: 512 for each tile of 256, 256 for each of 128. */
     if (s.tiles >= (s.side == 256 ? 1u << 23 : 1u << 24) || (rows && (lddy >= MAX_LD || x->ldq >= MAX_LD || x->lde >= MAX_LD))) return NSML_ECAP;
+    const Area out = area(dw, NSML_F32, n, lddw, k);
+    if (clash({out, area(need ? work : nullptr, 1, 0, need)},
+              {area(dy, type, rows, lddy, n), codes_area(x, rows, k), exps_area(x, rows, k), floats(col_scale, k), apart(area(add, NSML_F32, n, lddw, k), out)}))
+        return NSML_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
     /* Large results past the caches, where dy and x are read from, if their rows are whole lines (8192 x 11008 x 4096: 764 -> 728 us; see
      * the products for rows that are not). */

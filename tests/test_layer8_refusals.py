@@ -186,3 +186,82 @@ def test_tall_products_of_few_columns_beyond_a_launch(m, n):
 def test_weight_gradients_beyond_a_launch(n, k):
     """2^23 tiles of 256 have 2^32 threads."""
     refused(L.nsml_ckpt8_wgrad(P, 1, n, ck(ldq=k, lde=k // 32), None, 3, n, k, None, P, k, P, 1 << 40, None), nsml.ECAP)
+
+
+# ---------------------------------------------------------------- buffers that share bytes
+
+A = [1 << 20 << i for i in range(12)]       # addresses far apart; nothing is read from them
+
+
+def free(rc):
+    """Not refused: without a GPU the launch itself fails.  (Never run where there is one: the addresses are nobody's.)"""
+    assert rc == nsml.EHIP
+
+
+CALLS = {
+    # name of each buffer: bytes from row to row, rows, bytes of a row; then which are written, and the call
+    "q8_rows": ({"x": 128, "col": 256, "q": 64, "s": 12}, "q s",
+                lambda b: L.nsml_q8_rows(b["x"], 1, 64, 3, 64, b["col"], b["q"], 64, b["s"], None)),
+    "q8_values": ({"q": 64, "s": 12, "out": 128}, "out", lambda b: L.nsml_q8_values(b["q"], 64, b["s"], 3, 64, b["out"], 1, 64, None)),
+    "q8_matmul": ({"a": 64, "sa": 12, "b": 64, "sb": 20, "bias": 20, "c": 10}, "c",
+                  lambda b: L.nsml_q8_matmul(b["a"], 64, b["sa"], b["b"], 64, b["sb"], b["bias"], 3, 5, 64, b["c"], 1, 5, None)),
+    "ckpt8_pack": ({"x": 128, "q": 64, "e": 2}, "q e", lambda b: L.nsml_ckpt8_pack(b["x"], 1, 64, 3, 64, ck(b["q"], b["e"]), None)),
+    "ckpt8_unpack": ({"q": 64, "e": 2, "out": 128}, "out", lambda b: L.nsml_ckpt8_unpack(ck(b["q"], b["e"]), 3, 64, b["out"], 1, 64, None)),
+    "ckpt8_wgrad": ({"dy": 2000, "q": 64, "e": 2, "col": 256, "dw": 256, "work": 1 << 16}, "dw work",
+                    lambda b: L.nsml_ckpt8_wgrad(b["dy"], 1, 1000, ck(b["q"], b["e"]), b["col"], 4000, 1000, 64, None, b["dw"], 64, b["work"], 1 << 40, None)),
+    "rmsnorm_q8": ({"x": 128, "r": 128, "g": 256, "h": 128, "q": 64, "s": 12, "rstd": 12, "xq": 64, "xe": 2}, "h q s rstd xq xe",
+                   lambda b: L.nsml_rmsnorm_q8(b["x"], 64, b["r"], 64, b["g"], 1e-5, 1, 3, 64, b["h"], 64, b["q"], 64, b["s"], b["rstd"], ck(b["xq"], b["xe"]), None)),
+    "rmsnorm_backward": ({"dy": 128, "q": 64, "e": 2, "rstd": 12, "g": 256, "dres": 128, "dx": 128, "dg": 256, "work": 256}, "dx dg work",
+                         lambda b: L.nsml_rmsnorm_backward(b["dy"], 64, ck(b["q"], b["e"]), b["rstd"], b["g"], b["dres"], 64, 1, 3, 64, b["dx"], 64, b["dg"],
+                                                           b["work"], 1 << 40, None)),
+    "swiglu_q8": ({"g": 128, "u": 128, "q": 64, "s": 12, "gq": 64, "ge": 2, "uq": 64, "ue": 2, "aq": 64, "ae": 2}, "q s gq ge uq ue aq ae",
+                  lambda b: L.nsml_swiglu_q8(b["g"], 64, b["u"], 64, 1, 3, 64, b["q"], 64, b["s"], ck(b["gq"], b["ge"]), ck(b["uq"], b["ue"]), ck(b["aq"], b["ae"]), None)),
+    "swiglu_backward": ({"da": 128, "gq": 64, "ge": 2, "uq": 64, "ue": 2, "dg": 128, "du": 128}, "dg du",
+                        lambda b: L.nsml_swiglu_backward(b["da"], 64, ck(b["gq"], b["ge"]), ck(b["uq"], b["ue"]), 1, 3, 64, b["dg"], 64, b["du"], 64, None)),
+}
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="calls that are not refused have addresses of nobody's")
+@pytest.mark.parametrize("name", CALLS)
+def test_buffers_that_share_bytes(name):
+    width, written, call = CALLS[name]
+    apart = dict(zip(width, A))
+    free(call(apart))
+    for w in written.split():
+        for other in width:
+            if other == w:
+                continue
+            # what is written begins in the first row of the other one, or ends in it
+            last = 16 if width[other] > 16 else 0
+            for at in (apart[other] + last, apart[other] - 16 if width[w] > 16 else apart[other]):
+                refused(call({**apart, w: at}))
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="calls that are not refused have addresses of nobody's")
+def test_buffers_that_may_be_the_same_or_lie_side_by_side():
+    for name, same in (("rmsnorm_q8", ("h", "x")), ("rmsnorm_q8", ("h", "r")), ("rmsnorm_backward", ("dx", "dy")), ("rmsnorm_backward", ("dx", "dres")),
+                       ("swiglu_backward", ("dg", "da")), ("swiglu_backward", ("du", "da"))):
+        width, _, call = CALLS[name]
+        b = dict(zip(width, A))
+        free(call({**b, same[0]: b[same[1]]}))
+    # halves of one matrix, in either order, and one half that reaches into the other
+    def halves(dg, du, ld, da=A[0]):
+        return L.nsml_swiglu_backward(da, 64, ck(A[1], A[2]), ck(A[3], A[4]), 1, 3, 64, dg, ld, du, ld, None)
+    free(halves(A[5], A[5] + 128, 128))
+    free(halves(A[5] + 128, A[5], 128))
+    refused(halves(A[5], A[5] + 128, 127))
+    refused(halves(A[5], A[5] + 126, 128))
+    # a sum over micro-batches in place, beside it, or shifted
+    def wg(add, dw=A[4], lddw=64):
+        return L.nsml_ckpt8_wgrad(A[0], 1, 1000, ck(A[1], A[2]), None, 3, 1000, 64, add, dw, lddw, A[6], 1 << 40, None)
+    free(wg(A[4]))
+    free(wg(A[4] + 256, lddw=128))
+    refused(wg(A[4] + 256))
+    # a checkpoint whose exponents stand behind the codes of each row, and rows of other pitches between them
+    free(L.nsml_ckpt8_pack(A[0], 1, 64, 3, 64, ck(A[1], A[1] + 64, 80, 80), None))
+    refused(L.nsml_ckpt8_pack(A[0], 1, 64, 3, 64, ck(A[1], A[1] + 63, 80, 80), None))
+    free(L.nsml_ckpt8_pack(A[0], 1, 64, 3, 64, ck(A[1], A[1] + 64, 80, 160), None))
+    refused(L.nsml_ckpt8_pack(A[0], 1, 64, 3, 64, ck(A[1], A[1] + 64, 80, 60), None))
+    # scales in the gap behind the only row that they meet
+    free(L.nsml_q8_rows(A[0], 1, 64, 3, 64, None, A[1], 80, A[1] + 64, None))
+    refused(L.nsml_q8_rows(A[0], 1, 64, 3, 64, None, A[1], 64, A[1] + 64, None))
