@@ -320,6 +320,8 @@ int nsml_q8_rows(const void *x, int type, uint64_t ldx, uint64_t rows, uint32_t 
 /* Back: out (type) = q * scale[row]; scale NULL: 1. */
 int nsml_q8_values(const int8_t *q, uint64_t ldq, const float *scale, uint64_t rows, uint32_t cols,
                    void *out, int type, uint64_t ldo, void *stream);
+/* The codes the other way round: out[c, r] = q[r, c] (cols x rows, ldo bytes from row to row; a code matrix as well, rows up to 2^31 - 256). */
+int nsml_q8_transpose(const int8_t *q, uint64_t ldq, uint64_t rows, uint32_t cols, int8_t *out, uint64_t ldo, void *stream);
 
 /* c[i, j] (type, m x n) = a_scale[i] * b_scale[j] * sum_k a[i, k] * b[j, k] + bias[j]: a product with weights held by
  * output channel (n x k).  The sum is exact.  b_scale, bias (dev, float[n]) may be NULL (1 and 0); k <=

@@ -456,6 +456,7 @@ _f32c, _ck = C.c_float, C.POINTER(_CkptArg)
 for _name, _args in {
     "nsml_q8_rows": [_vp, _i32, _u64, _u64, _u32, _vp, _vp, _u64, _vp, _vp],
     "nsml_q8_values": [_vp, _u64, _vp, _u64, _u32, _vp, _i32, _u64, _vp],
+    "nsml_q8_transpose": [_vp, _u64, _u64, _u32, _vp, _u64, _vp],
     "nsml_q8_matmul": [_vp, _u64, _vp, _vp, _u64, _vp, _vp, _u64, _u32, _u32, _vp, _i32, _u64, _vp],
     "nsml_ckpt8_pack": [_vp, _i32, _u64, _u64, _u32, _ck, _vp],
     "nsml_ckpt8_unpack": [_ck, _u64, _u32, _vp, _i32, _u64, _vp],
@@ -650,9 +651,10 @@ def q8_rows(x: torch.Tensor, col_scale: Optional[torch.Tensor] = None, out: Opti
 def q8_transposed(w: Q8) -> Q8:
     """The codes of w the other way round, without scales: what the gradient of the data is multiplied by,
     q8_matmul(q8_rows(dc, col_scale=w.scale), q8_transposed(w)).  A layout to make once per update of the weights."""
-    _, _, n, k, _ = _rows_of("w", w, _device_of("w.q", w.q))
-    out = _new_codes(k, n, w.q.device)
-    out.copy_(w.q.t())
+    dev = _device_of("w.q", w.q)
+    q, ldq, n, k, _ = _rows_of("w", w, dev)
+    out = _new_codes(k, n, dev)
+    _enqueue(dev, _lib.nsml_q8_transpose, q, ldq, n, k, out.data_ptr(), (n + 15) & ~15)
     return Q8(out, None)
 
 

@@ -265,3 +265,13 @@ def test_buffers_that_may_be_the_same_or_lie_side_by_side():
     # scales in the gap behind the only row that they meet
     free(L.nsml_q8_rows(A[0], 1, 64, 3, 64, None, A[1], 80, A[1] + 64, None))
     refused(L.nsml_q8_rows(A[0], 1, 64, 3, 64, None, A[1], 64, A[1] + 64, None))
+
+
+def test_transpose():
+    def tr(q=P, ldq=64, m=48, k=64, out=1 << 20, ldo=48):
+        return L.nsml_q8_transpose(q, ldq, m, k, out, ldo, None)
+    for bad in ({"q": None}, {"q": P + 8}, {"ldq": 48}, {"ldq": 72}, {"k": 0}, {"out": None}, {"out": P + 4}, {"ldo": 32}, {"ldo": 56}, {"out": P}, {"out": P + 48 * 64 - 16}):
+        refused(tr(**bad))
+    refused(tr(k=(1 << 32) - 1, ldq=1 << 32), nsml.ECAP)
+    refused(tr(m=1 << 31, ldo=1 << 31), nsml.ECAP)
+    assert L.nsml_q8_transpose(None, 0, 0, 64, None, 0, None) == nsml.OK
