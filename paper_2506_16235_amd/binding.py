@@ -444,6 +444,8 @@ def decompress(ctx: Context, idx, val, scales, n, bucket_off, ratio, bits, out=N
 
 
 # ----------------------------------------------------------------------- the 8-bit layer
+#
+# The gradients are calls of their own, and no result has a graph: tensors that require one are refused while torch records.
 
 Q8_MAX_COLS, NORM_MAX_COLS = 131072, 32768
 
@@ -502,6 +504,7 @@ class GluQ8(NamedTuple):
 
 _TYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _F32_ONLY, _I8_ONLY, _U8_ONLY = torch.float32, torch.int8, torch.uint8
+_recording = torch.is_grad_enabled
 
 
 def _matrix(name, t, dev, dtype=None, rows=None, cols=None, _Tensor=torch.Tensor):
@@ -513,7 +516,8 @@ def _matrix(name, t, dev, dtype=None, rows=None, cols=None, _Tensor=torch.Tensor
             ld, side = t.stride()
             if ((t.dtype in _TYPE if dtype is None else t.dtype is dtype) and t.device == dev and c
                     and (rows is None or r == rows) and (cols is None or c == cols)
-                    and (side == 1 or c == 1 or not r) and (ld >= c or r <= 1)):
+                    and (side == 1 or c == 1 or not r) and (ld >= c or r <= 1)
+                    and not (t.requires_grad and _recording())):
                 return t.data_ptr(), (ld if ld > c else c), r, c
     raise ValueError(_why_not(name, t, dev, dtype, rows, cols))
 
@@ -533,7 +537,14 @@ def _why_not(name, t, dev, dtype, rows, cols) -> str:
         return f"{name} is {r} x {c}, needs {r if rows is None else rows} x {c if cols is None else cols}"
     if c == 0:
         return f"{name} has no columns"
+    if t.requires_grad and _recording():
+        return _no_graph(name)
     return f"{name} has strides {t.stride()}: rows must be contiguous and must not overlap"
+
+
+def _no_graph(name) -> str:
+    return (f"{name} requires a gradient, and results of the 8-bit layer have no graph: call under torch.no_grad(), "
+            "or from the forward of a torch.autograd.Function")
 
 
 def _vector(name, t, dev, n, _Tensor=torch.Tensor):
@@ -541,6 +552,8 @@ def _vector(name, t, dev, n, _Tensor=torch.Tensor):
     if t is None:
         return None
     if isinstance(t, _Tensor) and t.dtype is _F32_ONLY and t.shape == (n,) and t.device == dev and t.is_contiguous():
+        if t.requires_grad and _recording():
+            raise ValueError(_no_graph(name))
         return t.data_ptr()
     raise ValueError(f"{name} must be a contiguous float32 vector of {n} elements on {dev}")
 

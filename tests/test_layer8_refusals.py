@@ -275,3 +275,29 @@ def test_transpose():
     refused(tr(k=(1 << 32) - 1, ldq=1 << 32), nsml.ECAP)
     refused(tr(m=1 << 31, ldo=1 << 31), nsml.ECAP)
     assert L.nsml_q8_transpose(None, 0, 0, 64, None, 0, None) == nsml.OK
+
+
+def test_binding_refuses_what_wants_a_graph():
+    """Results have none: a gradient would be missing without a word."""
+    m, v = torch.zeros(4, 40, requires_grad=True), torch.zeros(5, requires_grad=True)
+    for t in (m, m[:, :30], m * 2):
+        with pytest.raises(ValueError, match="requires a gradient"):
+            nsml._matrix("x", t, CPU)
+    with pytest.raises(ValueError, match="requires a gradient"):
+        nsml._vector("v", v, CPU, 5)
+    with torch.no_grad():
+        assert nsml._matrix("x", m, CPU)[1:] == (40, 4, 40) and nsml._vector("v", v, CPU, 5) == v.data_ptr()
+    assert nsml._matrix("x", m.detach(), CPU)[0] == m.data_ptr()
+
+    class Norm(torch.autograd.Function):            # how a training program calls them
+        @staticmethod
+        def forward(ctx, x):
+            nsml._matrix("x", x, CPU)
+            return x.clone()
+
+        @staticmethod
+        def backward(ctx, dy):
+            nsml._matrix("dy", dy, CPU)
+            return dy
+    (Norm.apply(m) * torch.ones(4, 40)).sum().backward()
+    assert (m.grad == 1).all()
