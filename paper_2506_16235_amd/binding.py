@@ -619,6 +619,9 @@ def _device_of(name, t) -> torch.device:
     return t.device
 
 
+_written = torch.autograd.graph.increment_version       # torch does not see that the library writes a tensor of the caller's
+
+
 def _result(name, out, rows, cols, dtype, dev):
     """-> (matrix to write, address, elements from row to row): the caller's, or a new one."""
     if out is None:
@@ -627,6 +630,7 @@ def _result(name, out, rows, cols, dtype, dev):
         out = _mat(rows, cols, dtype, dev)
         return out, out.data_ptr(), cols
     at, ld, _, _ = _matrix(name, out, dev, None, rows, cols)
+    _written(out)
     return out, at, ld
 
 
@@ -657,6 +661,7 @@ def q8_rows(x: torch.Tensor, col_scale: Optional[torch.Tensor] = None, out: Opti
         q, ldq, _, _, s = _rows_of("out", out, dev, m, k)
         if s is None:
             raise ValueError("out.scale is required")
+        _written(out)
     _enqueue(dev, _lib.nsml_q8_rows, at, _TYPE[x.dtype], ld, m, k, col, q, ldq, s)
     return out
 
@@ -702,6 +707,7 @@ def ckpt8_pack(x: torch.Tensor, out: Optional[Ckpt8] = None) -> Ckpt8:
         out, arg = _new_ckpt(m, k, dev)
     else:
         arg = _ckpt("out", out, dev, m, k)[0]
+        _written(out)
     _enqueue(dev, _lib.nsml_ckpt8_pack, at, _TYPE[x.dtype], ld, m, k, arg)
     return out
 
@@ -780,6 +786,7 @@ def rmsnorm_backward(dy: torch.Tensor, xhat: Ckpt8, rstd: torch.Tensor, gamma: O
         dg = dgamma.data_ptr()
     else:
         dg = _vector("dgamma", dgamma, dev, k)
+        _written(dgamma)
     need = _lib.nsml_rmsnorm_backward_work(m, k)
     work = _vec(need, _uint8, dev)
     _enqueue(dev, _lib.nsml_rmsnorm_backward, at, ld, arg, rs, g, d, ldd, _TYPE[dy.dtype], m, k, o, ldo, dg, work.data_ptr(), need)

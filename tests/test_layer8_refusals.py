@@ -301,3 +301,35 @@ def test_binding_refuses_what_wants_a_graph():
             return dy
     (Norm.apply(m) * torch.ones(4, 40)).sum().backward()
     assert (m.grad == 1).all()
+
+
+def test_binding_tells_torch_what_it_writes(monkeypatch):
+    """A tensor that torch has kept for a backward pass and the library then writes has to fail there, not to give a wrong gradient."""
+    monkeypatch.setattr(nsml, "_device_of", lambda name, t: t.device)
+    monkeypatch.setattr(nsml, "_enqueue", lambda dev, fn, *args: None)
+    x, f32 = torch.zeros(4, 48), torch.float32
+    q, _, _ = _aligned(4, 48)
+    c, r = nsml.Ckpt8(q, torch.zeros(4, 2, dtype=torch.uint8)), nsml.Q8(q, torch.ones(4))
+
+    def rises(call, *tensors):
+        before = [t._version for t in tensors]
+        call(*tensors)
+        assert all(t._version > v for t, v in zip(tensors, before))
+    code, scale, e = _aligned(4, 48)[0], torch.zeros(4), torch.zeros(4, 2, dtype=torch.uint8)
+    rises(lambda *_: nsml.q8_rows(x, out=nsml.Q8(code, scale)), code, scale)
+    rises(lambda *_: nsml.ckpt8_pack(x, out=nsml.Ckpt8(code, e)), code, e)
+    rises(lambda o: nsml.q8_values(r, out=o), torch.zeros(4, 48))
+    rises(lambda o: nsml.ckpt8_unpack(c, out=o), torch.zeros(4, 48))
+    rises(lambda o: nsml.q8_matmul(r, r, out=o), torch.zeros(4, 4))
+    rises(lambda o: nsml.ckpt8_wgrad(x, c, out=o), torch.zeros(48, 48))
+    rises(lambda o, d: nsml.rmsnorm_backward(x, c, torch.ones(4), out=o, dgamma=d), torch.zeros(4, 48), torch.zeros(48))
+    rises(lambda a, b: nsml.swiglu_backward(x, c, c, dgate=a, dup=b), torch.zeros(4, 48), torch.zeros(4, 48))
+    flat = torch.zeros(2 * 48 * 48)
+    rises(lambda f: nsml.ckpt8_wgrad(x, c, out=f[48 * 48:].view(48, 48)), flat)
+    # and in earnest
+    w = torch.ones(4, 4, requires_grad=True)
+    kept = torch.ones(4, 4)
+    loss = (w * kept).sum()
+    nsml.q8_matmul(r, r, out=kept, dtype=f32)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
