@@ -619,6 +619,17 @@ def _device_of(name, t) -> torch.device:
     return t.device
 
 
+def _device_of_codes(name, x, kind) -> torch.device:
+    if not isinstance(x, kind):
+        raise ValueError(f"{name} must be a {kind.__name__}")
+    return _device_of(name + ".q", x.q)
+
+
+def _same_type(name, out, dtype):
+    if isinstance(out, torch.Tensor) and out.dtype != dtype:
+        raise ValueError(f"{name} has dtype {out.dtype}, not {dtype}")
+
+
 _written = torch.autograd.graph.increment_version       # torch does not see that the library writes a tensor of the caller's
 
 
@@ -669,7 +680,7 @@ def q8_rows(x: torch.Tensor, col_scale: Optional[torch.Tensor] = None, out: Opti
 def q8_transposed(w: Q8) -> Q8:
     """The codes of w the other way round, without scales: what the gradient of the data is multiplied by,
     q8_matmul(q8_rows(dc, col_scale=w.scale), q8_transposed(w)).  A layout to make once per update of the weights."""
-    dev = _device_of("w.q", w.q)
+    dev = _device_of_codes("w", w, Q8)
     q, ldq, n, k, _ = _rows_of("w", w, dev)
     out = _new_codes(k, n, dev)
     _enqueue(dev, _lib.nsml_q8_transpose, q, ldq, n, k, out.data_ptr(), (n + 15) & ~15)
@@ -678,7 +689,7 @@ def q8_transposed(w: Q8) -> Q8:
 
 def q8_values(x: Q8, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The values that 8-bit rows stand for."""
-    dev = _device_of("x.q", x.q)
+    dev = _device_of_codes("x", x, Q8)
     q, ldq, m, k, s = _rows_of("x", x, dev)
     out, at, ld = _result("out", out, m, k, dtype, dev)
     _enqueue(dev, _lib.nsml_q8_values, q, ldq, s, m, k, at, _TYPE[out.dtype], ld)
@@ -688,7 +699,7 @@ def q8_values(x: Q8, dtype: torch.dtype = torch.float32, out: Optional[torch.Ten
 def q8_matmul(a: Q8, b: Q8, dtype: torch.dtype = torch.bfloat16, bias: Optional[torch.Tensor] = None,
               out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """a (m x k) times b (n x k, weights by output channel) transposed, plus bias (float32 [n]); the sum is exact."""
-    dev = _device_of("a.q", a.q)
+    dev = _device_of_codes("a", a, Q8)
     qa, lda, m, k, sa = _rows_of("a", a, dev)
     qb, ldb, n, _, sb = _rows_of("b", b, dev, None, k)
     if sa is None:
@@ -714,7 +725,7 @@ def ckpt8_pack(x: torch.Tensor, out: Optional[Ckpt8] = None) -> Ckpt8:
 
 def ckpt8_unpack(x: Ckpt8, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The values that a checkpoint stands for."""
-    dev = _device_of("x.q", x.q)
+    dev = _device_of_codes("x", x, Ckpt8)
     arg, m, k = _ckpt("x", x, dev)
     out, at, ld = _result("out", out, m, k, dtype, dev)
     _enqueue(dev, _lib.nsml_ckpt8_unpack, arg, m, k, at, _TYPE[out.dtype], ld)
@@ -729,8 +740,7 @@ def ckpt8_wgrad(dy: torch.Tensor, x: Ckpt8, col_scale: Optional[torch.Tensor] = 
     at, ld, m, n = _matrix("dy", dy, dev)
     arg, _, k = _ckpt("x", x, dev, m)
     col = _vector("col_scale", col_scale, dev, k)
-    if out is not None and out.dtype != _float32:
-        raise ValueError(f"out has dtype {out.dtype}")
+    _same_type("out", out, _float32)
     out, w, ldw = _result("out", out, n, k, _float32, dev)
     base = None
     if add is not None:
@@ -778,8 +788,7 @@ def rmsnorm_backward(dy: torch.Tensor, xhat: Ckpt8, rstd: torch.Tensor, gamma: O
     d, ldd = None, 0
     if dres is not None:
         d, ldd, _, _ = _matrix("dres", dres, dev, dy.dtype, m, k)
-    if out is not None and out.dtype != dy.dtype:
-        raise ValueError(f"out has dtype {out.dtype}")
+    _same_type("out", out, dy.dtype)
     out, o, ldo = _result("out", out, m, k, dy.dtype, dev)
     if dgamma is None:
         dgamma = _vec(k, _float32, dev)
@@ -811,9 +820,8 @@ def swiglu_backward(da: torch.Tensor, gate: Ckpt8, up: Ckpt8, dgate: Optional[to
     dev = _device_of("da", da)
     at, ld, m, k = _matrix("da", da, dev)
     kg, ku = _ckpt("gate", gate, dev, m, k)[0], _ckpt("up", up, dev, m, k)[0]
-    for name, t in (("dgate", dgate), ("dup", dup)):
-        if t is not None and t.dtype != da.dtype:
-            raise ValueError(f"{name} has dtype {t.dtype}")
+    _same_type("dgate", dgate, da.dtype)
+    _same_type("dup", dup, da.dtype)
     dgate, g, ldg = _result("dgate", dgate, m, k, da.dtype, dev)
     dup, u, ldu = _result("dup", dup, m, k, da.dtype, dev)
     _enqueue(dev, _lib.nsml_swiglu_backward, at, ld, kg, ku, _TYPE[da.dtype], m, k, g, ldg, u, ldu)

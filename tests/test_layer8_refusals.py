@@ -333,3 +333,17 @@ def test_binding_tells_torch_what_it_writes(monkeypatch):
     nsml.q8_matmul(r, r, out=kept, dtype=f32)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.backward()
+
+
+def test_binding_refuses_other_things_with_its_own_error(monkeypatch):
+    x = torch.zeros(4, 32)
+    for call in (lambda: nsml.q8_values(x), lambda: nsml.q8_transposed(x), lambda: nsml.q8_matmul(x, x), lambda: nsml.ckpt8_unpack(x), lambda: nsml.q8_values(None)):
+        with pytest.raises(ValueError, match="must be a (Q8|Ckpt8)"):
+            call()
+    monkeypatch.setattr(nsml, "_device_of", lambda name, t: t.device)
+    q, _, _ = _aligned(4, 32)
+    c = nsml.Ckpt8(q, torch.zeros(4, 1, dtype=torch.uint8))
+    for call in (lambda: nsml.ckpt8_wgrad(x, c, out="out"), lambda: nsml.rmsnorm_backward(x, c, torch.ones(4), out=3.0),
+                 lambda: nsml.swiglu_backward(x, c, c, dgate=[1]), lambda: nsml.swiglu_backward(x, c, c, dup=(x, x))):
+        with pytest.raises(ValueError):
+            call()
