@@ -291,8 +291,10 @@ template <int MR, int NC> int go_few(const int8_t *a, uint64_t lda, const int8_t
     k_product_few<MR, NC, W><<<dim3((n + NC * 16 - 1) / (NC * 16), (uint32_t)((m + MR * 16 - 1) / (MR * 16))), W * 64, 0, st>>>(a, lda, b, ldb, m, n, k, out);
     return launched();
 }
-/* As many rows of b to a workgroup as give every compute unit one workgroup (us for 16, 32, 48 and 64 rows, k = 4096: 1 x 4096 6.3, 7.4, 9.1, 10.8;
- * 48 x 4096 11.5, 12.9, 15.5, 17.5; 1 x 11008 13.3, 15.4, 13.1, 15.2).  More than 32 rows of a come here only where 32 of b do. */
+/* As many rows of b to a workgroup as give every compute unit one workgroup (us for 16, 32, 48 and 64 rows, k = 4096: 1 x 4096 7.1, 8.7, 10.7, 13.2;
+ * 48 x 4096 12.8, 14.5; 1 x 11008 13.2, 15.6, 13.4, 15.5).  More than 32 rows of a come here only where 32 of b do.  These figures and those below:
+ * both operands of so many matrices in turn that they come from memory, results in bfloat16, 24 calls in a graph (weights that stay in the last cache:
+ * 1 x 11008 10.7, 48 x 11008 in tiles 15.2). */
 template <int MR, typename... A> int few_cols(uint64_t nc, A... x)
 {
     if (nc <= 1) return go_few<MR, 1>(x...);
@@ -312,10 +314,10 @@ int launch_few(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb, uin
 }
 
 /* Whether k is split over the wavefronts of a workgroup.  Up to 64 rows, unless there are so many rows of b that tiles fill the chip and
- * their ring in LDS keeps more on its way (us, split and in tiles; k = 4096: 1 x 11008 14, 15; 48 x 11008 20, 18; 64 x 4096 14, 14;
- * 16 x 32000 36, 33; 64 x 32000 65, 37).  Beyond that where there are few tiles (512 x 512 x 4096 12, 14; 128 x 768 x 11008 27, 32; 171 x 1500 x
- * 5184 13, 17; 1868 x 179 x 2112, 90 tiles, 8.1, 9.2; 6000 x 64 x 4096, 94, 17, 14; 128 x 4096 x 4096 15, 14) and k is not short (623 x 384 x 517
- * 4.5, 5.2; 152 x 1939 x 80 5.7, 4.5; 83 x 3060 x 256 5.8, 4.7). */
+ * their ring in LDS keeps more on its way (us, split and in tiles; k = 4096: 1 x 11008 13.4, 15.3; 48 x 11008 28.5, 17.3; 64 x 4096 15.1, 16.6;
+ * 16 x 32000 36.0, 31.4; 64 x 32000 68, 37.5).  Beyond that where there are few tiles (512 x 512 x 4096 12.4, 14.3; 128 x 768 x 11008 26.9, 32.0;
+ * 171 x 1500 x 5184 14.5, 17.2; 1868 x 179 x 2112, 90 tiles, 8.9, 9.5; 6000 x 64 x 4096, 94, 19.0, 19.6; 128 x 4096 x 4096, 128, 16.8, 19.6, but 15
+ * and 14 with a in the caches) and k is not short (623 x 384 x 517 4.7, 5.4; 152 x 1939 x 80 5.8, 3.9; 83 x 3060 x 256 5.9, 4.6). */
 bool by_few(uint64_t m, uint32_t n, uint32_t k)
 {
     const uint64_t tiles = ((m + 63) / 64) * ((n + 63) / 64);
@@ -338,11 +340,12 @@ int launch_product(const int8_t *a, uint64_t lda, const int8_t *b, uint64_t ldb,
      * but 8192 x 5001 x 512 40 -> 56. */
     out.past = m > 64 && large >= 96 && whole_lines(out.c, out.ldc * sizeof(T));
     /* The largest tiles that still give work to most compute units (us by tiles of 256, halved where they are few, 128 and 64: 2048 x 4096 x 4096
-     * 48, 52, 84; 1024 x 4096 x 4096 30, 25, 41; 4096 x 768 x 768 11, 9.3, 10; 1024 x 1536 x 1536 15, 11.5, 10; 6459 x 768 x 2877, 78 of 256, 27,
-     * 31, 37; 5579 x 617 x 1792, 66, 18, 15, 20).  Where k is short, those of 64 as long as the chip holds all of them at a time (5596 x 704 x 97
-     * 8.4, 8.5, 6.2; 279 x 6592 x 640 -, 9.0, 6.6; 4715 x 768 x 768 10.2, 10.0, 11.5; 7819 x 779 x 192 9.6, 10.3, 10.3; 6463 x 896 x 576 11.8,
-     * 11.4, 13.1).  Where the weights are read once, from memory, the ring is twice as long (48 x 11008 x 4096 20.4 -> 18.3).  No side is longer
-     * than the matrix needs (100 x 32000 x 4096 36, 25, 38; 40000 x 128 x 4096 51, 41, 50; 100000 x 64 x 1024 45, 30, 23). */
+     * 46.5, 51, 85; 1024 x 4096 x 4096 41.5, 29.5, 43.8; 4096 x 768 x 768 11.2, 9.4, 10.0; 1024 x 1536 x 1536 15.6, 11.8, 10.1; 6459 x 768 x 2877, 78
+     * of 256, 35.9, 35.1, 43; 5579 x 617 x 1792, 66, 20.2, 17.0, 21.0).  Where k is short, those of 64 as long as the chip holds all of them at a time
+     * (5596 x 704 x 97 8.8, 8.9, 6.4; 279 x 6592 x 640 10.8, 9.3, 7.7; 4715 x 768 x 768 11.5, 9.9, 11.9; 7819 x 779 x 192 9.6, 10.3, 10.3;
+     * 6463 x 896 x 576 12.2, 12.4, 14.0).  Where the weights are read once, from memory, the ring is twice as long (48 x 11008 x 4096 20.7 -> 17.3).
+     * No side is longer than the matrix needs (100 x 32000 x 4096 48.6, 34.2, 51.1; 40000 x 128 x 4096 63.6, 59.1, 66.4; 100000 x 64 x 1024 50.8,
+     * 37.1, 33.8). */
     const bool wide = m > 128 && n > 128 && large >= 76;
     if (m <= 64)
         k_product<T, 64, 8><<<(uint32_t)tiles(64), 256, 0, st>>>(a, lda, b, ldb, m, n, k, out);

@@ -126,8 +126,9 @@ template <int T, int V, typename OP> int go_rows(const OP &op, uint64_t rows, ui
 }
 /* A wavefront holds rows of up to 1024 columns, four up to 4096, eight up to 8192; beyond that as many as the operator's registers make
  * best: with few registers each, workgroups share a compute unit and one reads while the other computes, with more, less of them wait
- * at a row's barrier (rows of 11008, us for 1024 x 2, 768 x 2, 512 x 3, 256 x 6 threads times eights: gated activation of 4096 with
- * checkpoints 117, 77, 86, 126; norm of 8192 with its checkpoint 211 (768), 175 (512), 200 (256); codes alone 61, 49, 45, 50). */
+ * at a row's barrier (rows of 11008 bfloat16 from memory, us for 1024 x 2, 768 x 2, 512 x 3, 256 x 6 threads times eights: gated activation of 4096 with
+ * checkpoints 106, 80, 87, 125, of 8192 without 144, 97, 110, 168; q8_rows of 8192 with col_scale 70, 69, 67, 70; norm of 8192 with its checkpoint
+ * 208, 151, 173, 199: there 512 was chosen when the norm took more registers). */
 template <typename OP> int launch_rows(const OP &op, uint64_t rows, uint32_t cols, hipStream_t st)
 {
     if (rows == 0) return NSML_OK;
@@ -238,14 +239,14 @@ template <typename T> struct OpNorm {
 };
 
 /* 1 / (1 + exp(-x)) by the GPU's exponential of two and reciprocal (a unit in the last place each); 0 and 1 at the infinities, 0 below 2^-126.
- * What is lost in rounding x log2(e), and what log2(e) lacks as binary32, the exponential turns into 1.25 |x| units of 2^-24: `rough` is within
- * (5 + 1.25 |x|) 2^-24 of the value, enough for what becomes codes (half a step is 2^-8 of a row's absmax). */
+ * What is lost in rounding x log2(e), and what log2(e) lacks as binary32, the exponential turns into 1.25 |x| units of 2^-24: this one is within
+ * (5 + 1.25 |x|) 2^-24 of the value, enough for what becomes codes (half a step is 2^-8 of a row's absmax).  Measured at -20: 14.2 units, by `sigmoid` 3.1. */
 __device__ __forceinline__ float sigmoid_rough(float x)
 {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -0x1.715476p+0f));
 }
 /* For gradients, which may be binary32: the rest of that product goes into a factor 1 + rest * ln 2.  Within 7 * 2^-24, for four
- * instructions more (the gradient takes no longer for them; the activation by `rough`, 4096 x 11008 without checkpoints, 52.0 us, by this 53.6). */
+ * instructions more (the gradient takes no longer for them; the activation by the rough one, 4096 x 11008 without checkpoints, 52.0 us, by this 53.6). */
 __device__ __forceinline__ float sigmoid(float x)
 {
     const float v = __builtin_amdgcn_fmed3f(x, -200.0f, 200.0f);
@@ -368,7 +369,8 @@ template <typename T> struct OpGluBack {
 
 /* out[c, r] = q[r, c] by tiles of 128 x 128: 16 bytes of a row per lane into LDS, then 16 rows of four columns per thread, turned round by
  * permutations of bytes, and 16 bytes of a row out.  Eight lanes read, and write, a line of 128 bytes.  Rows of LDS are 33 words apart, the second
- * 64 eight words further, so that the 64 words that a wavefront reads lie in as many banks.  Bound by memory (11008 x 4096: 15.0 us, 6.0 TB/s). */
+ * 64 eight words further, so that the 64 words that a wavefront reads lie in as many banks.  Bound by memory (11008 x 4096: 22.0 us
+ * from memory, 4.1 TB/s, 15.0 where the codes are still in the last cache). */
 __global__ void __launch_bounds__(256) k_turn(const int8_t *q, uint64_t ldq, int8_t *out, uint64_t ldo, uint32_t rows, uint32_t cols)
 {
     __shared__ uint32_t tile[128 * 33 + 8];
