@@ -295,8 +295,8 @@ int nsml_last_l2norm(nsml_ctx *ctx, double *total, double *per_bucket);
  *   code matrices   16-byte aligned, ld a multiple of 16; the bytes of a row up to the next multiple of 16
  *             belong to it (their contents are never used as values, and may be overwritten)
  * NSML_EINVAL: a null pointer, an unknown type, cols == 0, ld < cols, a code matrix or pointer that is not aligned
- * as above, buffers that share bytes where one of them is written (unless said otherwise; parts of one matrix side by side share none);
- * NSML_ECAP: cols beyond the limit named (2^31 - 256 if none is), an ld of a product's or weight gradient's
+ * as above, buffers that share bytes where one of them is written (unless said otherwise; parts of one matrix side by
+ * side share none); NSML_ECAP: cols beyond the limit named (2^31 - 256 if none is), an ld of a product's or weight gradient's
  * operand beyond 2^22, a result of theirs of more tiles than one launch has (of 256 x 256, about 2^23; for products of up
  * to 64 rows or columns about 2^24 of 64 x 64; for weight gradients with a side up to 128 about 2^24 of 128 x 128);
  * NSML_EHIP: the launch failed. */
@@ -320,8 +320,10 @@ int nsml_q8_rows(const void *x, int type, uint64_t ldx, uint64_t rows, uint32_t 
 /* Back: out (type) = q * scale[row]; scale NULL: 1. */
 int nsml_q8_values(const int8_t *q, uint64_t ldq, const float *scale, uint64_t rows, uint32_t cols,
                    void *out, int type, uint64_t ldo, void *stream);
-/* The codes the other way round: out[c, r] = q[r, c] (cols x rows, ldo bytes from row to row; a code matrix as well, rows up to 2^31 - 256). */
-int nsml_q8_transpose(const int8_t *q, uint64_t ldq, uint64_t rows, uint32_t cols, int8_t *out, uint64_t ldo, void *stream);
+/* The codes the other way round: out[c, r] = q[r, c] (cols x rows, ldo bytes from row to row; a code matrix as well, rows
+ * up to 2^31 - 256). */
+int nsml_q8_transpose(const int8_t *q, uint64_t ldq, uint64_t rows, uint32_t cols, int8_t *out, uint64_t ldo,
+                      void *stream);
 
 /* c[i, j] (type, m x n) = a_scale[i] * b_scale[j] * sum_k a[i, k] * b[j, k] + bias[j]: a product with weights held by
  * output channel (n x k).  The sum is exact.  b_scale, bias (dev, float[n]) may be NULL (1 and 0); k <=
@@ -353,10 +355,11 @@ int nsml_ckpt8_wgrad(const void *dy, int type, uint64_t lddy, const nsml_ckpt8 *
 /* Root-mean-square norm with the residual's addition, in 8 bits:
  *   h = x + residual (type, rounded; both NULL: h is x)       rstd = 1 / sqrt(mean of h^2 over the row + eps)
  *   (q, scale) = rows of gamma * h * rstd                     xhat = checkpoint of h * rstd (or NULL)
- * gamma: dev, float[cols], or NULL for 1.  rstd: dev, out, float[rows].  h may be x or residual itself.  Codes do not depend on how the mean was rounded:
- * they are those of gamma * h, and rstd goes into the scale: the absmax of gamma * h is what has to be 2^-112 or more for codes other than 0,
- * and finite.  h^2 may leave binary32's range; rstd ends at its largest value, so that a row of zeros without eps has scale 0, a
- * checkpoint of zeros and, where dy is 0, a gradient of 0.  cols <= NSML_NORM_MAX_COLS. */
+ * gamma: dev, float[cols], or NULL for 1.  rstd: dev, out, float[rows].  h may be x or residual itself.
+ * Codes do not depend on how the mean was rounded: they are those of gamma * h, and rstd goes into the scale; the absmax of
+ * gamma * h is what has to be 2^-112 or more for codes other than 0, and finite.  h^2 may leave binary32's range.  rstd ends
+ * at its largest value, so that a row of zeros without eps has scale 0, a checkpoint of zeros and, where dy is 0, a gradient
+ * of 0.  cols <= NSML_NORM_MAX_COLS. */
 int nsml_rmsnorm_q8(const void *x, uint64_t ldx, const void *residual, uint64_t ldr, const float *gamma, float eps,
                     int type, uint64_t rows, uint32_t cols, void *h, uint64_t ldh, int8_t *q, uint64_t ldq,
                     float *scale, float *rstd, const nsml_ckpt8 *xhat, void *stream);
