@@ -99,7 +99,8 @@ k_attend(Attend<T> g)
     };
     const uint32_t block0 = FEW ? wave * 32u : 0u;
     Clean cleaner(lds + 4 * TILE);
-    /* all: every row of the wavefront sees every key of its blocks.  marked: values of some keys are not finite. */
+    /* all: every row of the wavefront sees every key of its blocks, and none is marked.  marked: values of some keys are not finite, and zeros in LDS for
+     * every wavefront, whether it sees all of the tile or not. */
     auto work = [&](uint32_t t, const uint8_t *in, bool all, bool marked) INLINE {
         const uint32_t key0 = t * KB + block0;
         const Shared in_k = shared(in) + block0 * L::ROW, in_v = in_k + TILE;
@@ -165,7 +166,7 @@ k_attend(Attend<T> g)
         const bool mixed = t * KB < end.lo || (t + 1u) * KB > first.lo + first.count, marked = mixed && cleaner.template clean<1>(in + TILE);
         const uint32_t a = t * KB + block0, z = a + BLOCKS * 32u;
         if (wr > last || z <= wave_first.lo || a >= wave_end.lo + wave_end.count) return;
-        work(t, in, a >= wave_end.lo && z <= wave_first.lo + wave_first.count, marked);
+        work(t, in, !marked && a >= wave_end.lo && z <= wave_first.lo + wave_first.count, marked);
     };
     if (from < to) fetch(from, lds);
     for (uint32_t t = from; t < to; t += 2u) {
