@@ -443,8 +443,8 @@ int nsml_rotary(const nsml_heads *q, uint32_t q_heads, const nsml_heads *k, uint
  *   rest       0, or 1 for o and 2 for lse, added up
  *   work       dev, 16-byte aligned, nsml_attention_work(...) bytes (may be 0), not kept
  * Scores, maxima and sums are in binary32; weights are rounded to `type` before they meet the values.  Keys and values
- * that a query does not see have no part in its result, whatever they hold; values that it sees with a weight other than 0 and that are not finite make
- * it, in their column at least, NaN or infinite. */
+ * that a query does not see have no part in its result, whatever they hold; values that it sees and that are not finite make it, in their column at
+ * least, NaN or infinite, also where their weight is too small for binary32.  lse is made of scores alone. */
 uint64_t nsml_attention_work(int type, uint64_t q_rows, uint64_t k_rows, uint32_t seqs, uint32_t heads, uint32_t kv_heads, uint32_t dim);
 int nsml_attention(const nsml_heads *q, const nsml_heads *k, const nsml_heads *v, int type, const nsml_seqs *seqs, uint32_t heads,
                    uint32_t kv_heads, uint32_t dim, int32_t left, int32_t right, float scale, const nsml_heads *o, float *lse, int rest,

@@ -437,7 +437,8 @@ __device__ __forceinline__ Seen seen_by(const Reach &r, const Seq &s, uint32_t q
 /* ---------------------------------------------------------------- values that are not finite where nobody sees them
  *
  * A product over rows takes a row that somebody does not see with weight 0, and 0 times an infinity is NaN.  So in tiles of which not everybody sees
- * everything such values become zeros in LDS, and their rows are marked: whoever sees one of those with a weight other than 0 has that made NaN. */
+ * everything such values become zeros in LDS, for all wavefronts, and their rows are marked: whoever sees one of those, in a wavefront that sees all of the tile
+ * or not, has its result made NaN at the end. */
 template <typename T, int D, int ROWS, int THREADS> struct Cleaner {
     typedef TileOf<T, D> L;
     static constexpr int BYTES = ROWS * 4 + 16;
@@ -480,6 +481,15 @@ template <typename T, int D, int ROWS, int THREADS> struct Cleaner {
     }
     /* Marks of rows 8 x to 8 x + 3 from row `first` on, of this lane's half. */
     __device__ __forceinline__ float of(uint32_t first, int e, uint32_t lane) const { return mark[first + acc_row(e, lane)]; }
+    /* NaN, or 0: whether this lane's half of the 32 rows from `first` on, of which it sees those numbered below `count` from `at` on, has a marked row that
+     * it sees.  By itself, apart from the products: marks among the weights took 27 registers of a prompt's loop. */
+    __device__ __forceinline__ float seen(uint32_t first, uint32_t at, uint32_t count, uint32_t lane) const
+    {
+        float any = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; e++) any += at + acc_row(e, lane) < count ? of(first, e, lane) : 0.0f;
+        return any;
+    }
 };
 
 /* ---------------------------------------------------------------- softmax */

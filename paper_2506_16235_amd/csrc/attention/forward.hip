@@ -99,9 +99,9 @@ k_attend(Attend<T> g)
     };
     const uint32_t block0 = FEW ? wave * 32u : 0u;
     Clean cleaner(lds + 4 * TILE);
-    /* all: every row of the wavefront sees every key of its blocks, and none is marked.  marked: values of some keys are not finite, and zeros in LDS for
-     * every wavefront, whether it sees all of the tile or not. */
-    auto work = [&](uint32_t t, const uint8_t *in, bool all, bool marked) INLINE {
+    float none = 0.0f;                           /* NaN when a value that was made zero in LDS is seen by this lane's row */
+    /* all: every row of the wavefront sees every key of its blocks. */
+    auto work = [&](uint32_t t, const uint8_t *in, bool all) INLINE {
         const uint32_t key0 = t * KB + block0;
         const Shared in_k = shared(in) + block0 * L::ROW, in_v = in_k + TILE;
         v16f p[BLOCKS] = {};
@@ -112,11 +112,6 @@ k_attend(Attend<T> g)
                 if (used<T, D, R>(i * 16, g.dim)) mma(at_k(in_k, b * 32u, i), q[i], p[b]);
         __builtin_amdgcn_sched_barrier(0);
         if (!all) {
-            if (marked)
-#pragma unroll
-                for (int b = 0; b < BLOCKS; b++)
-#pragma unroll
-                    for (int e = 0; e < 16; e++) p[b][e] += cleaner.of(block0 + b * 32u, e, lane);
             uint32_t first = key0 + lane / 32u * 4u - seen.lo;
             asm("" : "+v"(first));               /* one register and what a row adds, not a register for each row */
 #pragma unroll
@@ -166,14 +161,20 @@ k_attend(Attend<T> g)
         const bool mixed = t * KB < end.lo || (t + 1u) * KB > first.lo + first.count, marked = mixed && cleaner.template clean<1>(in + TILE);
         const uint32_t a = t * KB + block0, z = a + BLOCKS * 32u;
         if (wr > last || z <= wave_first.lo || a >= wave_end.lo + wave_end.count) return;
-        work(t, in, !marked && a >= wave_end.lo && z <= wave_first.lo + wave_first.count, marked);
+        if (marked)
+#pragma unroll
+            for (int b = 0; b < BLOCKS; b++) none += cleaner.seen(block0 + b * 32u, a + b * 32u - seen.lo, seen.count, lane);
+        work(t, in, a >= wave_end.lo && z <= wave_first.lo + wave_first.count);
     };
     if (from < to) fetch(from, lds);
     for (uint32_t t = from; t < to; t += 2u) {
         turn(t, lds, lds + 2 * TILE);
         if (t + 1u < to) turn(t + 1u, lds + 2 * TILE, lds);
     }
-    sum = half_sum(sum);
+    sum = half_sum(sum), none = half_sum(none);
+    if (__ballot(none != 0.0f))
+#pragma unroll
+        for (int b = 0; b < DB; b++) o[b] += none;
 
     if constexpr (FEW) {
         /* Everybody's maximum and sums, then the sums brought to the largest and added up in the order of the wavefronts, each by one for its columns. */

@@ -89,3 +89,15 @@ def test_a_value_shows_in_results(dt, dim, heads, kv, m, n, causal, window):
         p = Pack(dt, dim, heads, kv, m, n, causal, window, places)
         got = nsml.attention(p.q, p.k, p.spoiled(p.v, n, kv - 1), p.seqs, **p.how)
         p.shown(got.o, p.clean.o, m, p.of_head(p.who_sees(), heads, slice((kv - 1) * p.group, None)), f"o, {len(places)} sequences")
+
+
+@types
+@dims
+@groups
+@pytest.mark.parametrize("m,n,causal,window", SHAPES + TOKENS)
+def test_a_value_has_no_part_in_lse(dt, dim, heads, kv, m, n, causal, window):
+    """lse is made of scores alone."""
+    for places in packs(n, range(max(128, n - 64), n)):
+        p = Pack(dt, dim, heads, kv, m, n, causal, window, places)
+        got = nsml.attention(p.q, p.k, p.spoiled(p.v, n, 0), p.seqs, **p.how)
+        assert torch.equal(got.lse, p.clean.lse), (len(places), int((got.lse != p.clean.lse).sum()))
