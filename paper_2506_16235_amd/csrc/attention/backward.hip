@@ -350,7 +350,8 @@ __device__ __forceinline__ void grad_keys(const Grad<T> &g, const Job &job, uint
         }
     };
     Cleaner<T, D, QB, W * 64> cleaner(lds + 2 * STAGE);
-    auto work = [&](uint32_t t, const uint8_t *in, bool all, bool marked) INLINE {
+    float none = 0.0f;                               /* NaN when this lane's key is seen by a query of which a value was made zero in LDS */
+    auto work = [&](uint32_t t, const uint8_t *in, bool all) INLINE {
         const Shared in_q = shared(in), in_d = in_q + TILE, side = in_d + TILE + lane / 32u * 16u;
 #pragma unroll
         for (int b = 0; b < QB / 32; b++) {
@@ -376,13 +377,6 @@ __device__ __forceinline__ void grad_keys(const Grad<T> &g, const Job &job, uint
                 }
             }
             if (!all) {
-                if (marked)
-#pragma unroll
-                    for (int e = 0; e < 16; e++) {
-                        const float m = cleaner.of(b * 32u, e, lane);
-                        if constexpr (DV) w[e] += m;
-                        if constexpr (DK) ds[e] += m;
-                    }
                 uint32_t here = t * QB + b * 32u + lane / 32u * 4u - my_lo;
                 asm("" : "+v"(here));
 #pragma unroll
@@ -421,13 +415,23 @@ __device__ __forceinline__ void grad_keys(const Grad<T> &g, const Job &job, uint
         const uint32_t a = t * QB, z = a + QB;
         const bool mixed = a < first_all || z > end_all, marked = mixed && cleaner.template clean<2>(in);
         if (wk >= s.n || z <= any_lo || a >= any_hi) return;
-        work(t, in, a >= all_lo && z <= all_hi, marked);
+        if (marked)
+#pragma unroll
+            for (int b = 0; b < QB / 32; b++) none += cleaner.seen(b * 32u, a + b * 32u - my_lo, my_count, lane);
+        work(t, in, a >= all_lo && z <= all_hi);
     };
     if (from < to) fetch(from, lds);
     for (uint32_t t = from; t < to; t += 2u) {
         turn(t, lds, lds + STAGE);
         if (t + 1u < to) turn(t + 1u, lds + STAGE, lds);
     }
+    none = half_sum(none);
+    if (__ballot(none != 0.0f))
+#pragma unroll
+        for (int b = 0; b < DB; b++) {
+            if constexpr (DK) ak[b] += none;
+            if constexpr (DV) av[b] += none;
+        }
     if (wk + lane % 32u >= s.n) return;
     /* q was not scaled; in binary32 k was, but q is what dk is made of */
     const float fk = g.scale * power(-LIFT<T>) / level.up, fv = power(-LIFT<T>);

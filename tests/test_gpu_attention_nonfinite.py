@@ -101,3 +101,31 @@ def test_a_value_has_no_part_in_lse(dt, dim, heads, kv, m, n, causal, window):
         p = Pack(dt, dim, heads, kv, m, n, causal, window, places)
         got = nsml.attention(p.q, p.k, p.spoiled(p.v, n, 0), p.seqs, **p.how)
         assert torch.equal(got.lse, p.clean.lse), (len(places), int((got.lse != p.clean.lse).sum()))
+
+
+def gradients(p, **spoiled):
+    """Of the clean run's result and lse, with one of its tensors spoiled."""
+    t = {"do": p.do, "q": p.q, "k": p.k, "v": p.v, **spoiled}
+    return nsml.attention_backward(t["do"], t["q"], t["k"], t["v"], *p.clean, p.seqs, **p.how)
+
+
+@types
+@dims
+@groups
+@shapes
+@pytest.mark.parametrize("which", ["do", "q"])
+def test_a_query_or_its_gradient_shows_in_the_gradients_of_keys(dt, dim, heads, kv, m, n, causal, window, which):
+    for places in packs(m):
+        p = Pack(dt, dim, heads, kv, m, n, causal, window, places)
+        head = heads - 1
+        clean, got = gradients(p), gradients(p, **{which: p.spoiled(getattr(p, which), m, head)})
+        hit = p.of_head(p.who_is_seen(), kv, head // p.group)
+        if which == "do":
+            p.shown(got[2], clean[2], n, hit, "dv")
+            p.kept(got[1], clean[1], n, hit, "dk")
+        else:
+            p.shown(got[1], clean[1], n, hit, "dk")
+            p.kept(got[2], clean[2], n, hit, "dv")
+        own = torch.zeros(p.c, m, dtype=torch.bool, device=DEV)
+        own[range(p.c), places] = True
+        p.kept(got[0], clean[0], m, p.of_head(own, heads, head), "dq")
