@@ -453,6 +453,8 @@ int nsml_attention(const nsml_heads *q, const nsml_heads *k, const nsml_heads *v
  *   dq = scale * sum of ds[j] k[j]     dk[j] = scale * sum of ds[j] q     dv[j] = sum of p[j] dout
  * over the keys that a query sees, and the queries (of all heads that read it) that see a key.  dq, dk and dv may be parts of one matrix.
  * rest: 0, or 1 for dq, 2 for dk and 4 for dv, added up.
+ * Rows that are not seen have no part in a gradient, whatever they hold; seen ones that are not finite make it, in their column at least, NaN or
+ * infinite: k and v dq, q and dout dk, dout dv.
  * Sums are in binary32 in an order that sizes and lengths alone decide. */
 uint64_t nsml_attention_backward_work(int type, uint64_t q_rows, uint64_t k_rows, uint32_t seqs, uint32_t heads, uint32_t kv_heads, uint32_t dim);
 int nsml_attention_backward(const nsml_heads *dout, const nsml_heads *q, const nsml_heads *k, const nsml_heads *v, const nsml_heads *o, const float *lse,

@@ -479,16 +479,13 @@ template <typename T, int D, int ROWS, int THREADS> struct Cleaner {
         dirty = uniform(to_bits(mark[ROWS])) != 0;
         return dirty;
     }
-    /* Marks of rows 8 x to 8 x + 3 from row `first` on, of this lane's half. */
-    __device__ __forceinline__ float of(uint32_t first, int e, uint32_t lane) const { return mark[first + acc_row(e, lane)]; }
-    /* NaN, or 0: whether this lane's half of the 32 rows from `first` on, of which it sees those numbered below `count` from `at` on, has a marked row that
-     * it sees.  By itself, apart from the products: marks among the weights took 27 registers of a prompt's loop. */
-    __device__ __forceinline__ float seen(uint32_t first, uint32_t at, uint32_t count, uint32_t lane) const
+    /* NaN, or 0: whether one of the 32 rows from `first` on is marked, of which the lane sees those from lo up to hi (either may lie outside).  By itself, apart
+     * from the products: marks among the weights took 27 registers of a prompt's loop. */
+    __device__ __forceinline__ float seen(uint32_t first, int32_t lo, int32_t hi) const
     {
-        float any = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 16; e++) any += at + acc_row(e, lane) < count ? of(first, e, lane) : 0.0f;
-        return any;
+        const uint32_t marked = (uint32_t)__ballot(mark[first + threadIdx.x % 32u] != 0.0f);
+        const uint32_t below = (1ull << max(0, min(hi, 32))) - 1ull, before = (1ull << max(0, min(lo, 32))) - 1ull;
+        return marked & below & ~before ? from_bits(0x7FC00000u) : 0.0f;
     }
 };
 

@@ -141,8 +141,9 @@ k_attend_dq(Grad<T> g)
     };
     Cleaner<T, D, KB, W * 64> cleaner(lds + 4 * TILE);
     float over = 0.0f;                               /* this lane's part of the sum of ds */
+    float none = 0.0f;                               /* NaN when a key of which an element was made zero in LDS is seen by this lane's row */
     /* Weights and ds of 32 keys. */
-    auto scores = [&](uint32_t t, const uint8_t *in, int b, bool all, bool marked, float (&w)[16], float (&ds)[16]) INLINE {
+    auto scores = [&](uint32_t t, const uint8_t *in, int b, bool all, float (&w)[16], float (&ds)[16]) INLINE {
         v16f p = {}, dp = {};
 #pragma unroll
         for (int i = 0; i < D / 16; i++)
@@ -157,9 +158,6 @@ k_attend_dq(Grad<T> g)
             ds[e] = w[e] * (dp[e] - delta);
         }
         if (!all) {
-            if (marked)
-#pragma unroll
-                for (int e = 0; e < 16; e++) ds[e] += cleaner.of(b * 32u, e, lane);
             uint32_t here = t * KB + b * 32u + lane / 32u * 4u - seen.lo;
             asm("" : "+v"(here));                    /* one register and what a row adds, not a register for each row */
 #pragma unroll
@@ -170,7 +168,7 @@ k_attend_dq(Grad<T> g)
             }
         }
     };
-    /* All tiles by turns in both halves of LDS: work(tile, where it is, whether every row of the wavefront sees all of it, whether rows are marked). */
+    /* All tiles by turns in both halves of LDS: work(tile, where it is, whether every row of the wavefront sees all of it). */
     auto tiles = [&](auto work) INLINE {
         auto turn = [&](uint32_t t, uint8_t *in, uint8_t *other) INLINE {
             tile_sync();
@@ -178,7 +176,10 @@ k_attend_dq(Grad<T> g)
             const uint32_t a = t * KB, z = a + KB;
             const bool mixed = a < end.lo || z > first.lo + first.count, marked = mixed && cleaner.template clean<1>(in);
             if (wr > last || z <= wave_first.lo || a >= wave_end.lo + wave_end.count) return;
-            work(t, in, a >= wave_end.lo && z <= wave_first.lo + wave_first.count, marked);
+            if (marked)
+#pragma unroll
+                for (int b = 0; b < KB / 32; b++) none += cleaner.seen(b * 32u, seen.lo - a - b * 32u, seen.lo + seen.count - a - b * 32u);
+            work(t, in, a >= wave_end.lo && z <= wave_first.lo + wave_first.count);
         };
         if (from < to) fetch(from, lds);
         for (uint32_t t = from; t < to; t += 2u) {
@@ -188,25 +189,25 @@ k_attend_dq(Grad<T> g)
     };
     const float low = power(-LIFT<T>);
     if (TWICE && end.lo + end.count <= first.lo + EXACT) {
-        tiles([&](uint32_t t, const uint8_t *in, bool all, bool marked) INLINE {
+        tiles([&](uint32_t t, const uint8_t *in, bool all) INLINE {
 #pragma unroll 1
             for (int b = 0; b < KB / 32; b++) {
                 float w[16], ds[16];
-                scores(t, in, b, all, marked, w, ds);
+                scores(t, in, b, all, w, ds);
 #pragma unroll
                 for (int e = 0; e < 16; e++) over += ds[e];
             }
         });
-        delta += half_sum(over) * low;
+        delta += half_sum(over) * low + none;
         wg_sync();                                   /* nobody reads LDS any more */
     }
     v16f acc[DB] = {}, mean[MEND ? DB : 1] = {};
     Level<T> level;
-    tiles([&](uint32_t t, const uint8_t *in, bool all, bool marked) INLINE {
+    tiles([&](uint32_t t, const uint8_t *in, bool all) INLINE {
 #pragma unroll
         for (int b = 0; b < KB / 32; b++) {
             float w[16], ds[16];
-            scores(t, in, b, all, marked, w, ds);
+            scores(t, in, b, all, w, ds);
             if constexpr (MEND)
 #pragma unroll
                 for (int e = 0; e < 16; e++) over += ds[e];
@@ -232,7 +233,10 @@ k_attend_dq(Grad<T> g)
                 }
         }
     });
-    const float r_off = MEND ? half_sum(over) * low : 0.0f;
+    if (__ballot(none != 0.0f))
+#pragma unroll
+        for (int b = 0; b < DB; b++) acc[b] += none;
+    const float r_off = MEND ? half_sum(over) * low + none : 0.0f;
     if (wr + lane % 32u > last) return;
     if (lane < 32u && job.split == 0) g.delta[row * g.heads + head] = delta + r_off;
     const float f = g.scale * low / level.up, fm = g.scale * low * r_off;
@@ -417,7 +421,7 @@ __device__ __forceinline__ void grad_keys(const Grad<T> &g, const Job &job, uint
         if (wk >= s.n || z <= any_lo || a >= any_hi) return;
         if (marked)
 #pragma unroll
-            for (int b = 0; b < QB / 32; b++) none += cleaner.seen(b * 32u, a + b * 32u - my_lo, my_count, lane);
+            for (int b = 0; b < QB / 32; b++) none += cleaner.seen(b * 32u, my_lo - a - b * 32u, my_lo + my_count - a - b * 32u);
         work(t, in, a >= all_lo && z <= all_hi);
     };
     if (from < to) fetch(from, lds);
@@ -425,7 +429,6 @@ __device__ __forceinline__ void grad_keys(const Grad<T> &g, const Job &job, uint
         turn(t, lds, lds + STAGE);
         if (t + 1u < to) turn(t + 1u, lds + STAGE, lds);
     }
-    none = half_sum(none);
     if (__ballot(none != 0.0f))
 #pragma unroll
         for (int b = 0; b < DB; b++) {

@@ -163,7 +163,7 @@ k_attend(Attend<T> g)
         if (wr > last || z <= wave_first.lo || a >= wave_end.lo + wave_end.count) return;
         if (marked)
 #pragma unroll
-            for (int b = 0; b < BLOCKS; b++) none += cleaner.seen(block0 + b * 32u, a + b * 32u - seen.lo, seen.count, lane);
+            for (int b = 0; b < BLOCKS; b++) none += cleaner.seen(block0 + b * 32u, seen.lo - a - b * 32u, seen.lo + seen.count - a - b * 32u);
         work(t, in, a >= wave_end.lo && z <= wave_first.lo + wave_first.count);
     };
     if (from < to) fetch(from, lds);
@@ -171,7 +171,7 @@ k_attend(Attend<T> g)
         turn(t, lds, lds + 2 * TILE);
         if (t + 1u < to) turn(t + 1u, lds + 2 * TILE, lds);
     }
-    sum = half_sum(sum), none = half_sum(none);
+    sum = half_sum(sum);
     if (__ballot(none != 0.0f))
 #pragma unroll
         for (int b = 0; b < DB; b++) o[b] += none;

@@ -129,3 +129,32 @@ def test_a_query_or_its_gradient_shows_in_the_gradients_of_keys(dt, dim, heads, 
         own = torch.zeros(p.c, m, dtype=torch.bool, device=DEV)
         own[range(p.c), places] = True
         p.kept(got[0], clean[0], m, p.of_head(own, heads, head), "dq")
+
+
+@types
+@dims
+@groups
+@shapes
+@pytest.mark.parametrize("which", ["k", "v"])
+def test_a_key_or_its_value_shows_in_the_gradient_of_queries(dt, dim, heads, kv, m, n, causal, window, which):
+    for places in packs(n):
+        p = Pack(dt, dim, heads, kv, m, n, causal, window, places)
+        clean, got = gradients(p), gradients(p, **{which: p.spoiled(getattr(p, which), n, kv - 1)})
+        p.shown(got[0], clean[0], m, p.of_head(p.who_sees(), heads, slice((kv - 1) * p.group, None)), "dq")
+
+
+@types
+@dims
+@shapes
+def test_a_value_goes_through_a_step(dt, dim, m, n, causal, window):
+    """Forward and backward together: what belongs to queries that do not see it, and keys that none of those sees that do, stays."""
+    p = Pack(dt, dim, 2, 2, m, n, causal, window, [*range(0, 128, 3)])
+    v = p.spoiled(p.v, n, 1)
+    r = nsml.attention(p.q, p.k, v, p.seqs, **p.how)
+    got, clean = nsml.attention_backward(p.do, p.q, p.k, v, *r, p.seqs, **p.how), gradients(p)
+    sees = p.who_sees()
+    p.shown(got[0], clean[0], m, p.of_head(sees, 2, 1), "dq")
+    with_it = (sees.double() @ p.seen.double()) > 0
+    p.shown(got[1], clean[1], n, p.of_head(with_it, 2, 1), "dk")
+    assert torch.equal(got[2], clean[2])                # the weights do not know of values
+    say(NAME[dt], dim, m, n, int(sees.sum()), int(with_it.sum()))
