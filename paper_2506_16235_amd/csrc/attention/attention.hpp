@@ -479,14 +479,16 @@ template <typename T, int D, int ROWS, int THREADS> struct Cleaner {
         dirty = uniform(to_bits(mark[ROWS])) != 0;
         return dirty;
     }
-    /* NaN, or 0: whether one of the 32 rows from `first` on is marked, of which the lane sees those from lo up to hi (either may lie outside).  By itself, apart
-     * from the products: marks among the weights took 27 registers of a prompt's loop. */
-    __device__ __forceinline__ float seen(uint32_t first, int32_t lo, int32_t hi) const
+    /* The lanes that see a marked one of the 32 rows from `first` on, a bit each: a lane sees those from lo up to hi, which may lie outside.  By itself, apart
+     * from the products, and in a scalar register: marks among the weights took 27 registers of a prompt's loop. */
+    __device__ __forceinline__ uint64_t seen(uint32_t first, int32_t lo, int32_t hi) const
     {
         const uint32_t marked = (uint32_t)__ballot(mark[first + threadIdx.x % 32u] != 0.0f);
         const uint32_t below = (1ull << max(0, min(hi, 32))) - 1ull, before = (1ull << max(0, min(lo, 32))) - 1ull;
-        return marked & below & ~before ? from_bits(0x7FC00000u) : 0.0f;
+        return __ballot((marked & below & ~before) != 0);
     }
+    /* What such a lane's result becomes by addition. */
+    static __device__ __forceinline__ float none(uint64_t lanes) { return lanes >> threadIdx.x % 64u & 1u ? from_bits(0x7FC00000u) : 0.0f; }
 };
 
 /* ---------------------------------------------------------------- softmax */

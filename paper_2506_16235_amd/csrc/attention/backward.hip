@@ -83,7 +83,8 @@ k_attend_dq(Grad<T> g)
     typedef TileOf<T, D> L;
     constexpr int ROWS = W * 32, TILE = KB * L::ROW, DB = D / 32;
     constexpr bool MEND = sizeof(T) == 2 && D == 64, TWICE = sizeof(T) == 2 && D > 64;      /* binary32 rounds o no more than anything else */
-    __shared__ __align__(16) uint8_t lds[4 * TILE + Cleaner<T, D, KB, W * 64>::BYTES];
+    typedef Cleaner<T, D, KB, W * 64> Clean;
+    __shared__ __align__(16) uint8_t lds[4 * TILE + Clean::BYTES];
     const uint32_t wave = uniform(threadIdx.x / 64u), lane = threadIdx.x % 64u;
     const bool parts = sizeof(T) == 4 && g.key_splits > 1u;
     const Job job = job_of(blockIdx.x, g.kv, parts ? g.key_splits : 1u);
@@ -139,9 +140,9 @@ k_attend_dq(Grad<T> g)
         load.keys(in, k, g.k.ld, t * KB, s.n, g.dim);
         load.keys(in + TILE, v, g.v.ld, t * KB, s.n, g.dim);
     };
-    Cleaner<T, D, KB, W * 64> cleaner(lds + 4 * TILE);
+    Clean cleaner(lds + 4 * TILE);
     float over = 0.0f;                               /* this lane's part of the sum of ds */
-    float none = 0.0f;                               /* NaN when a key of which an element was made zero in LDS is seen by this lane's row */
+    uint64_t none = 0;                               /* lanes whose row sees a key of which an element was made zero in LDS */
     /* Weights and ds of 32 keys. */
     auto scores = [&](uint32_t t, const uint8_t *in, int b, bool all, float (&w)[16], float (&ds)[16]) INLINE {
         v16f p = {}, dp = {};
@@ -178,7 +179,7 @@ k_attend_dq(Grad<T> g)
             if (wr > last || z <= wave_first.lo || a >= wave_end.lo + wave_end.count) return;
             if (marked)
 #pragma unroll
-                for (int b = 0; b < KB / 32; b++) none += cleaner.seen(b * 32u, seen.lo - a - b * 32u, seen.lo + seen.count - a - b * 32u);
+                for (int b = 0; b < KB / 32; b++) none |= cleaner.seen(b * 32u, seen.lo - a - b * 32u, seen.lo + seen.count - a - b * 32u);
             work(t, in, a >= wave_end.lo && z <= wave_first.lo + wave_first.count);
         };
         if (from < to) fetch(from, lds);
@@ -198,7 +199,7 @@ k_attend_dq(Grad<T> g)
                 for (int e = 0; e < 16; e++) over += ds[e];
             }
         });
-        delta += half_sum(over) * low + none;
+        delta += half_sum(over) * low + Clean::none(none);
         wg_sync();                                   /* nobody reads LDS any more */
     }
     v16f acc[DB] = {}, mean[MEND ? DB : 1] = {};
@@ -233,10 +234,10 @@ k_attend_dq(Grad<T> g)
                 }
         }
     });
-    if (__ballot(none != 0.0f))
+    if (none)
 #pragma unroll
-        for (int b = 0; b < DB; b++) acc[b] += none;
-    const float r_off = MEND ? half_sum(over) * low + none : 0.0f;
+        for (int b = 0; b < DB; b++) acc[b] += Clean::none(none);
+    const float r_off = MEND ? half_sum(over) * low + Clean::none(none) : 0.0f;
     if (wr + lane % 32u > last) return;
     if (lane < 32u && job.split == 0) g.delta[row * g.heads + head] = delta + r_off;
     const float f = g.scale * low / level.up, fm = g.scale * low * r_off;
@@ -353,8 +354,9 @@ __device__ __forceinline__ void grad_keys(const Grad<T> &g, const Job &job, uint
             if (DK) side[QB + own] = delta[i];
         }
     };
-    Cleaner<T, D, QB, W * 64> cleaner(lds + 2 * STAGE);
-    float none = 0.0f;                               /* NaN when this lane's key is seen by a query of which a value was made zero in LDS */
+    typedef Cleaner<T, D, QB, W * 64> Clean;
+    Clean cleaner(lds + 2 * STAGE);
+    uint64_t none = 0;                               /* lanes whose key is seen by a query of which a value was made zero in LDS */
     auto work = [&](uint32_t t, const uint8_t *in, bool all) INLINE {
         const Shared in_q = shared(in), in_d = in_q + TILE, side = in_d + TILE + lane / 32u * 16u;
 #pragma unroll
@@ -421,7 +423,7 @@ __device__ __forceinline__ void grad_keys(const Grad<T> &g, const Job &job, uint
         if (wk >= s.n || z <= any_lo || a >= any_hi) return;
         if (marked)
 #pragma unroll
-            for (int b = 0; b < QB / 32; b++) none += cleaner.seen(b * 32u, my_lo - a - b * 32u, my_lo + my_count - a - b * 32u);
+            for (int b = 0; b < QB / 32; b++) none |= cleaner.seen(b * 32u, my_lo - a - b * 32u, my_lo + my_count - a - b * 32u);
         work(t, in, a >= all_lo && z <= all_hi);
     };
     if (from < to) fetch(from, lds);
@@ -429,11 +431,11 @@ __device__ __forceinline__ void grad_keys(const Grad<T> &g, const Job &job, uint
         turn(t, lds, lds + STAGE);
         if (t + 1u < to) turn(t + 1u, lds + STAGE, lds);
     }
-    if (__ballot(none != 0.0f))
+    if (none)
 #pragma unroll
         for (int b = 0; b < DB; b++) {
-            if constexpr (DK) ak[b] += none;
-            if constexpr (DV) av[b] += none;
+            if constexpr (DK) ak[b] += Clean::none(none);
+            if constexpr (DV) av[b] += Clean::none(none);
         }
     if (wk + lane % 32u >= s.n) return;
     /* q was not scaled; in binary32 k was, but q is what dk is made of */

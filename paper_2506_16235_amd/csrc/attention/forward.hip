@@ -99,7 +99,7 @@ k_attend(Attend<T> g)
     };
     const uint32_t block0 = FEW ? wave * 32u : 0u;
     Clean cleaner(lds + 4 * TILE);
-    float none = 0.0f;                           /* NaN when a value that was made zero in LDS is seen by this lane's row */
+    uint64_t none = 0;                           /* lanes whose row sees a value that was made zero in LDS */
     /* all: every row of the wavefront sees every key of its blocks. */
     auto work = [&](uint32_t t, const uint8_t *in, bool all) INLINE {
         const uint32_t key0 = t * KB + block0;
@@ -163,7 +163,7 @@ k_attend(Attend<T> g)
         if (wr > last || z <= wave_first.lo || a >= wave_end.lo + wave_end.count) return;
         if (marked)
 #pragma unroll
-            for (int b = 0; b < BLOCKS; b++) none += cleaner.seen(block0 + b * 32u, seen.lo - a - b * 32u, seen.lo + seen.count - a - b * 32u);
+            for (int b = 0; b < BLOCKS; b++) none |= cleaner.seen(block0 + b * 32u, seen.lo - a - b * 32u, seen.lo + seen.count - a - b * 32u);
         work(t, in, a >= wave_end.lo && z <= wave_first.lo + wave_first.count);
     };
     if (from < to) fetch(from, lds);
@@ -172,9 +172,9 @@ k_attend(Attend<T> g)
         if (t + 1u < to) turn(t + 1u, lds + 2 * TILE, lds);
     }
     sum = half_sum(sum);
-    if (__ballot(none != 0.0f))
+    if (none)
 #pragma unroll
-        for (int b = 0; b < DB; b++) o[b] += none;
+        for (int b = 0; b < DB; b++) o[b] += Clean::none(none);
 
     if constexpr (FEW) {
         /* Everybody's maximum and sums, then the sums brought to the largest and added up in the order of the wavefronts, each by one for its columns. */
