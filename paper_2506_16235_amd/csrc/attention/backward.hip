@@ -69,12 +69,17 @@ __device__ __forceinline__ float power(float e) { return __builtin_amdgcn_exp2f(
 
 /* ---------------------------------------------------------------- dq, and delta for the other kernel
  *
- * delta = do o has the rounding of o in it, which the gradient would show where a query sees few keys.  The sum of ds over a query's keys is 0 but for what
- * delta is off by.  MEND: that sum is made beside ds, and what it is off by times the sum of p k is taken off at the end: a product that reads nothing
- * more.  Where registers do not last for that (dim beyond 64 in 16 bits), the keys are gone through twice where a tile's queries see EXACT of them at most,
- * first for delta alone; with more keys the rounding of o is seldom seen (bfloat16, scores of deviation 1.4: dq of 1200 tokens is off by 0.24 % either way,
- * 0.25 % without, where rounding dq alone makes 0.17 %). */
+ * delta = do o has the rounding of o in it, which the gradient shows where a query's weight is on few keys.  The sum of ds over a query's keys is 0 but for what
+ * delta is off by, so it is made beside ds, and dk always gets a delta without that.  dq is off by as much times the sum of p k.  MEND: that sum is made too, a
+ * product that reads nothing more, and taken off at the end.  AGAIN, where registers do not last for it (dim beyond 64 in 16 bits): a tile of queries that see
+ * EXACT keys at most goes through them for delta alone first.  One that sees more makes dq, and its wavefronts make theirs anew where delta is off by more
+ * than STEPS, two steps of the type, of the root of the sum of ds^2 for some row.  Rounding o and weights alone makes 0.3 steps in the mean square of keys with
+ * normal scores, and one row in 60000 comes to two (dq of 1200 tokens in bfloat16 is off by 0.24 % either way; 0.37 % in place of 0.29 where keys have
+ * a mean as large as their deviation).  Those of a key with all but 0.001 of the weight come far beyond: off by 133 % with a delta that is never mended, 0.28 % so.  The
+ * sums take 1 % of a step of 8192 tokens; one tile that goes through its keys twice ends last where all are long (4096 tokens, 32 heads of 128: 790 -> 840 us). */
 constexpr uint32_t EXACT = 512;
+template <typename T> constexpr float STEPS = 0.015625f;         /* 2^-6 */
+template <> constexpr float STEPS<f16> = 0.001953125f;           /* 2^-9 */
 
 template <typename T, int D, int W, int KB, Rows R>
 __global__ void __launch_bounds__(W * 64, sizeof(T) == 2 ? 2 : 1)
@@ -82,7 +87,7 @@ k_attend_dq(Grad<T> g)
 {
     typedef TileOf<T, D> L;
     constexpr int ROWS = W * 32, TILE = KB * L::ROW, DB = D / 32;
-    constexpr bool MEND = sizeof(T) == 2 && D == 64, TWICE = sizeof(T) == 2 && D > 64;      /* binary32 rounds o no more than anything else */
+    constexpr bool MEND = sizeof(T) == 2 && D == 64, AGAIN = sizeof(T) == 2 && D > 64;      /* binary32 rounds o no more than anything else */
     typedef Cleaner<T, D, KB, W * 64> Clean;
     __shared__ __align__(16) uint8_t lds[4 * TILE + Clean::BYTES];
     const uint32_t wave = uniform(threadIdx.x / 64u), lane = threadIdx.x % 64u;
@@ -169,6 +174,7 @@ k_attend_dq(Grad<T> g)
             }
         }
     };
+    bool idle = wr > last;                           /* this wavefront only brings what the others work on */
     /* All tiles by turns in both halves of LDS: work(tile, where it is, whether every row of the wavefront sees all of it). */
     auto tiles = [&](auto work) INLINE {
         auto turn = [&](uint32_t t, uint8_t *in, uint8_t *other) INLINE {
@@ -176,7 +182,7 @@ k_attend_dq(Grad<T> g)
             if (t + 1u < to) fetch(t + 1u, other);
             const uint32_t a = t * KB, z = a + KB;
             const bool mixed = a < end.lo || z > first.lo + first.count, marked = mixed && cleaner.template clean<1>(in);
-            if (wr > last || z <= wave_first.lo || a >= wave_end.lo + wave_end.count) return;
+            if (idle || z <= wave_first.lo || a >= wave_end.lo + wave_end.count) return;
             if (marked)
 #pragma unroll
                 for (int b = 0; b < KB / 32; b++) none |= cleaner.seen(b * 32u, seen.lo - a - b * 32u, seen.lo + seen.count - a - b * 32u);
@@ -189,7 +195,19 @@ k_attend_dq(Grad<T> g)
         }
     };
     const float low = power(-LIFT<T>);
-    if (TWICE && end.lo + end.count <= first.lo + EXACT) {
+    /* Where this lane's row lies, made where it is needed, not kept in registers from tile to tile. */
+    const auto own_row = [&](uint32_t &own_head) INLINE {
+        uint32_t in = threadIdx.x % 32u;
+        asm("" : "+v"(in));
+        const uint32_t own = min(wr + in, last), at = g.group.div(own);
+        own_head = head0 + own - at * g.group.n;
+        return (uint64_t)s.q0 + at;
+    };
+    const bool few = end.lo + end.count <= first.lo + EXACT;
+    v16f acc[DB] = {}, mean[MEND ? DB : 1] = {};
+    Level<T> level;
+    float squares = 0.0f;                            /* this lane's part of the sum of ds^2 */
+    if (AGAIN && few) {
         tiles([&](uint32_t t, const uint8_t *in, bool all) INLINE {
 #pragma unroll 1
             for (int b = 0; b < KB / 32; b++) {
@@ -199,51 +217,84 @@ k_attend_dq(Grad<T> g)
                 for (int e = 0; e < 16; e++) over += ds[e];
             }
         });
-        delta += half_sum(over) * low + Clean::none(none);
-        wg_sync();                                   /* nobody reads LDS any more */
+        delta += half_sum(over) * low;
+        wg_sync();
     }
-    v16f acc[DB] = {}, mean[MEND ? DB : 1] = {};
-    Level<T> level;
-    tiles([&](uint32_t t, const uint8_t *in, bool all) INLINE {
+    auto pass = [&]() INLINE {
+        tiles([&](uint32_t t, const uint8_t *in, bool all) INLINE {
 #pragma unroll
-        for (int b = 0; b < KB / 32; b++) {
-            float w[16], ds[16];
-            scores(t, in, b, all, w, ds);
-            if constexpr (MEND)
+            for (int b = 0; b < KB / 32; b++) {
+                float w[16], ds[16];
+                scores(t, in, b, all, w, ds);
+                if constexpr (MEND || AGAIN)
 #pragma unroll
-                for (int e = 0; e < 16; e++) over += ds[e];
-            level.take(ds, acc);
-            Frag<T> fd[2], fw[2];
+                    for (int e = 0; e < 16; e++) over += ds[e];
+                if constexpr (AGAIN)
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                float x[8];
+                    for (int e = 0; e < 16; e++) squares = __builtin_fmaf(ds[e], ds[e], squares);
+                level.take(ds, acc);
+                Frag<T> fd[2], fw[2];
 #pragma unroll
-                for (int e = 0; e < 8; e++) x[e] = ds[h * 8 + e] * level.up;
-                fd[h] = rounded<T>(x);
-                fw[h] = rounded<T>(w + h * 8);
-            }
-            __builtin_amdgcn_sched_barrier(0);
+                for (int h = 0; h < 2; h++) {
+                    float x[8];
 #pragma unroll
-            for (int h = 0; h < 2; h++)
-#pragma unroll
-                for (int x = 0; x < DB; x++) {
-                    if (!used<T, D, R>(x * 32, g.dim)) continue;
-                    const Frag<T> f = at_col(shared(in), b * 32u + h * 16u, x);
-                    mma(f, fd[h], acc[x]);
-                    if constexpr (MEND) mma(f, fw[h], mean[x]);
+                    for (int e = 0; e < 8; e++) x[e] = ds[h * 8 + e] * level.up;
+                    fd[h] = rounded<T>(x);
+                    fw[h] = rounded<T>(w + h * 8);
                 }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int x = 0; x < DB; x++) {
+                        if (!used<T, D, R>(x * 32, g.dim)) continue;
+                        const Frag<T> f = at_col(shared(in), b * 32u + h * 16u, x);
+                        mma(f, fd[h], acc[x]);
+                        if constexpr (MEND) mma(f, fw[h], mean[x]);
+                    }
+            }
+        });
+    };
+    pass();
+    if (AGAIN && !few) {
+        /* A row that has no need stays as it is or makes the same bits once more, so that none depends on its neighbours. */
+        over = half_sum(over) * low;
+        const bool off = fabsf(over) > STEPS<T> * low * __builtin_sqrtf(half_sum(squares));
+        wg_sync();                                   /* nobody reads LDS any more */
+        uint32_t *const any = reinterpret_cast<uint32_t *>(lds);
+        const bool some = __ballot(off) != 0;
+        any[wave] = some;
+        wg_sync();
+        uint32_t somebody = 0;
+#pragma unroll
+        for (int w = 0; w < W; w++) somebody |= any[w];
+        wg_sync();
+        uint32_t own_head;
+        const uint64_t own = own_row(own_head) * g.heads + own_head;
+        if (lane < 32u && wr + lane <= last) g.delta[own] = delta + over + Clean::none(none);
+        if (uniform(somebody)) {
+            delta = off ? delta + over : delta;
+            idle |= !some;
+            if (!idle) {
+#pragma unroll
+                for (int b = 0; b < DB; b++) acc[b] = v16f{};
+                level = Level<T>{};
+            }
+            pass();
         }
-    });
+    }
     if (none)
 #pragma unroll
         for (int b = 0; b < DB; b++) acc[b] += Clean::none(none);
-    const float r_off = MEND ? half_sum(over) * low + Clean::none(none) : 0.0f;
+    const float r_off = MEND ? half_sum(over) * low : 0.0f;
     if (wr + lane % 32u > last) return;
-    if (lane < 32u && job.split == 0) g.delta[row * g.heads + head] = delta + r_off;
+    uint32_t own_head;
+    const uint64_t own = own_row(own_head);
+    if ((!AGAIN || few) && lane < 32u && job.split == 0) g.delta[own * g.heads + own_head] = delta + r_off + (MEND || AGAIN ? Clean::none(none) : 0.0f);
     const float f = g.scale * low / level.up, fm = g.scale * low * r_off;
-    T *dq = g.dq.at(row, head);
+    T *dq = g.dq.at(own, own_head);
     if constexpr (sizeof(T) == 4)
-        if (parts) dq = g.part + query_part_at(g.seqs.q_rows, g.heads, g.dim, job.split, row, head);
+        if (parts) dq = g.part + query_part_at(g.seqs.q_rows, g.heads, g.dim, job.split, own, own_head);
 #pragma unroll
     for (int b = 0; b < DB; b++)
 #pragma unroll
