@@ -277,7 +277,8 @@ template <typename T> __global__ void __launch_bounds__(256) k_attend_join(Atten
         float total = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; i++) total += sums[i][threadIdx.x];
-        g.o.at(row, head)[threadIdx.x] = (T)(sum == 0.0f ? 0.0f : total / sum);
+        /* no weight at all: 0, or NaN if a value that is seen is not finite, as without splits */
+        g.o.at(row, head)[threadIdx.x] = (T)(sum == 0.0f ? total * 0.0f : total / sum);
     }
     if (threadIdx.x == 0) g.lse[row * g.heads + head] = sum == 0.0f ? from_bits(0xFF800000u) : (top + __log2f(sum) - OFFSET<T>) * LN2;
 }

@@ -158,3 +158,16 @@ def test_a_value_goes_through_a_step(dt, dim, m, n, causal, window):
     p.shown(got[1], clean[1], n, p.of_head(with_it, 2, 1), "dk")
     assert torch.equal(got[2], clean[2])                # the weights do not know of values
     say(NAME[dt], dim, m, n, int(sees.sum()), int(with_it.sum()))
+
+
+@types
+@pytest.mark.parametrize("n", [40, 5000])
+def test_a_value_shows_where_every_weight_is_0(dt, n):
+    """Scores of -infinity alone: weights of 0, of which the product with what is not finite is NaN, whether the keys are split or not."""
+    q, k, v = tensor(gen(n), 1, 2, 64, dt).abs() + 0.1, tensor(gen(n + 1), n, 2, 64, dt), tensor(gen(n + 2), n, 2, 64, dt)
+    k[:, :, 7] = -math.inf
+    r = nsml.attention(q, k, v)
+    assert bool((r.o == 0).all()) and bool((r.lse == -math.inf).all())
+    v[n - 3, 1, 5] = math.inf
+    o = nsml.attention(q, k, v).o
+    assert bool(torch.isnan(o[0, 1, 5])) and bool((o[0, 0] == 0).all())
