@@ -456,7 +456,8 @@ int nsml_attention(const nsml_heads *q, const nsml_heads *k, const nsml_heads *v
  * Rows that are not seen have no part in a gradient, whatever they hold; seen ones that are not finite make it, in their column at least, NaN or
  * infinite: k and v dq, q and dout dk, dout dv.
  * p and ds are rounded to `type` before they meet dout, q and k.  The rounding of o has no part in a gradient but this: in dq of heads of
- * more than 64 elements in 16 bits, delta may be off by two steps of the type times the root of the sum of ds^2, for queries that see over 512 keys.
+ * more than 64 elements in 16 bits, delta may be off by two steps of the type times the root of the sum of ds^2, where a tile of queries (128 rows)
+ * sees over 512 keys.
  * Sums are in binary32 in an order that sizes and lengths alone decide. */
 uint64_t nsml_attention_backward_work(int type, uint64_t q_rows, uint64_t k_rows, uint32_t seqs, uint32_t heads, uint32_t kv_heads, uint32_t dim);
 int nsml_attention_backward(const nsml_heads *dout, const nsml_heads *q, const nsml_heads *k, const nsml_heads *v, const nsml_heads *o, const float *lse,

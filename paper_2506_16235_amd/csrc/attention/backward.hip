@@ -7,7 +7,7 @@
  * sizes alone decide: no atomics.  With few keys the queries are split, each split writes its sums in 32 bits, and k_grad_join adds them in order.
  *
  * Bound by the matrix instructions and what stands between them, two wavefronts on a SIMD at most (8192 tokens in documents of 351 to 4509, 32 heads of 128 over 8,
- * bfloat16: dq 309 us, dk and dv 616, join 30; 16 x 512 tokens, 12 heads of 64: dq 44, dk with dv 53).
+ * bfloat16: dq 317 us, dk and dv 611, join 30; 16 x 512 tokens, 12 heads of 64: dq 44, dk with dv 53).
  */
 #include "attention.hpp"
 
@@ -53,7 +53,7 @@ template <> struct Level<f16> {
         for (int e = 0; e < N; e++) most = fmaxf(most, fabsf(ds[e]));
         most = half_max(most);
         if (__ballot(most * up > 32768.0f)) {
-            /* the largest to 2^7, so that few that are larger follow; what is lost lies 2^-31 below it */
+            /* the largest to 2^7, so that few that are larger follow; what is lost lies 2^-32 below it, where a sum in binary32 holds nothing of it */
             const float now = most * up > 32768.0f ? from_bits((261u - min(to_bits(most) >> 23, 254u)) << 23) : up;
             const float f = now / up;
             up = now;
@@ -397,7 +397,7 @@ __device__ __forceinline__ void grad_keys(const Grad<T> &g, const Job &job, uint
         load.queries(in, pq, g.q.ld, g.q.hs, g.group, t * QB, rows, g.dim);
         load.queries(in + TILE, pd, g.d.ld, g.d.hs, g.group, t * QB, rows, g.dim);
         {
-            /* every thread, so that none branches: several bring the same */
+            /* every thread, so that none branches: several bring the same.  The stores wait for all that was asked for before. */
             const uint32_t own = threadIdx.x % QB, r = min(t * QB + own, rows - 1u), at = g.group.div(r);
             const uint64_t i = (uint64_t)at * g.heads + r - at * g.group.n;
             float *side = reinterpret_cast<float *>(in + 2 * TILE);

@@ -5,8 +5,8 @@
  * lane's own and its other half's; p leaves the registers as the operand of the second product.
  *
  * Prompts are bound by the matrix instructions, which wait while maxima and exponentials are made unless the other wavefront of the SIMD has products (8192 causal
- * tokens, 32 heads of 128 in bfloat16: 550 us, 1.0 Pflop/s; 32768 over 8 heads of keys 8.2 ms, 1.07); single tokens by memory (16 over 4096 to 16384 keys, 32
- * heads of 128 over 8: 134 us, 4.3 TB/s) or, when few, by a chain of dependent loads (one over 777 keys, 12 heads of 64: 8 us and 4 to join).
+ * tokens, 32 heads of 128 in bfloat16: 549 us, 1.0 Pflop/s; 32768 over 8 heads of keys 8.2 ms, 1.07); single tokens by memory (16 over 4096 to 16384 keys, 32
+ * heads of 128 over 8: 135 us, 4.3 TB/s) or, when few, by a chain of dependent loads (one over 777 keys, 12 heads of 64: 8 us and 4 to join).
  */
 #include "attention.hpp"
 
@@ -154,7 +154,8 @@ k_attend(Attend<T> g)
             for (int d = 0; d < DB; d++)
                 if (used<T, D, R>(d * 32, g.dim)) mma(at_v(in_v, b * 16u, d), w[b], o[d]);
     };
-    /* One tile in the half of LDS that `in` is; the next one is asked for as soon as nobody reads the other half. */
+    /* One tile in the half of LDS that `in` is; the next one is asked for as soon as nobody reads the other half.  In 16 bits the compiler waits for it before the
+     * transposing reads of this one. */
     auto turn = [&](uint32_t t, uint8_t *in, uint8_t *other) INLINE {
         tile_sync();
         if (t + 1u < to) fetch(t + 1u, other);
